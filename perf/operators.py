@@ -46,13 +46,12 @@ def listed():
         # the default rollout batch with trees of 16 nodes
         dict(name="attention_b64_n16", op="attention", **qwen, page=16, batch=64, nodes=16, ctx_lo=1024, ctx_hi=4096,
              ragged=False),
-        # trees of up to 64 nodes: 256 query rows per KV head
+        # the largest trees over long contexts: up to 256 query rows per KV head
         dict(name="attention_b32_n64", op="attention", **qwen, page=32, batch=32, nodes=64, ctx_lo=512, ctx_hi=8704,
              ragged=True),
-        # long contexts
-        dict(name="attention_long_n8", op="attention", **qwen, page=16, batch=32, nodes=8, ctx_lo=16384, ctx_hi=32768,
-             ragged=False),
-        # the whole cache of the 36-layer Qwen3-4B configuration
+        # one interactive sequence: all launches and latency
+        dict(name="commit_b1_l36", op="commit", **qwen, page=16, batch=1, nodes=8, ctx_lo=50, ctx_hi=50, layers=36),
+        # a rollout batch in the whole cache of the 36-layer Qwen3-4B configuration
         dict(name="commit_b64_l36", op="commit", **qwen, page=16, batch=64, nodes=16, ctx_lo=16, ctx_hi=128, layers=36),
         # a decode step's rows with the alternatives that a draft tree is grown from
         dict(name="logprobs_b64_top8", op="logprobs", dtype="f32", rows=64, vocab=151936, temperature=1.0, topk=8,
@@ -66,7 +65,6 @@ def listed():
         # a policy update's rows as bf16 logits, with an entropy bonus
         dict(name="grad_m4096_bf16", op="logprobs_grad", dtype="bf16", rows=4096, vocab=151936, temperature=1.0,
              entropy=True),
-        # (the commit of one sequence stands among the drawn cases: it is as long as its launches)
     ]
 
 
