@@ -192,7 +192,8 @@ def _cache(c, seed, layers, lens, extra):
     need = (lens + extra + c["page"] - 1) // c["page"]
     need = np.maximum(need, 1)
     perm = _rng(seed, "pages").permutation(int(need.sum()))
-    table = np.full((len(lens), int(need.max())), -1, np.int32)
+    width = -(-(int(lens.max()) + int(np.max(extra))) // c["page"])       # room for the longest and the most rows
+    table = np.full((len(lens), max(1, width)), -1, np.int32)
     ends = np.cumsum(need)
     for b, n in enumerate(need):
         table[b, :n] = perm[ends[b] - n:ends[b]]
