@@ -6,7 +6,9 @@
  * sequence in one forward (gm_verify_forward, gm_verify_attention), accepts a
  * prefix of the k drafts and draws one more token (gm_spec_accept), commits
  * the accepted KV entries and rolls back the rest (gm_kv_commit), and the MTP
- * draft head proposes the next block (gm_mtp_draft).
+ * draft head proposes the next block (gm_mtp_draft).  Beside the chain stand
+ * the operators of draft trees (gm_kv_append, gm_tree_*) and of token
+ * log-probabilities (gm_token_logprobs and its gradient).
  *
  * Conventions shared by every entry point
  * ---------------------------------------
@@ -51,7 +53,7 @@ typedef enum {
   GM_ERR_DEVICE = -5         /* a HIP runtime call failed */
 } gm_status;
 
-enum { GM_DEVERR_TOKEN = 1, GM_DEVERR_PAGE = 2 };
+enum { GM_DEVERR_TOKEN = 1, GM_DEVERR_PAGE = 2, GM_DEVERR_TREE = 4 };
 
 typedef enum { GM_F32 = 0, GM_BF16 = 1 } gm_dtype;
 typedef enum { GM_GREEDY = 0, GM_SAMPLE = 1 } gm_accept_mode;
@@ -61,7 +63,9 @@ typedef enum {
   GM_OP_SPEC_ACCEPT = 2,
   GM_OP_MTP_DRAFT = 3,
   GM_OP_DCA_LOSS = 4,    /* B = cycles N, k = draft length K, cfg->vocab = V */
-  GM_OP_MTP_RECONSTRUCT = 5   /* B = cycles R, k = depth K, max_ctx = the cache's max_ctx */
+  GM_OP_MTP_RECONSTRUCT = 5,  /* B = cycles R, k = depth K, max_ctx = the cache's max_ctx */
+  GM_OP_TREE_ATTENTION = 6,   /* k = nodes N of a tree, 1..64 */
+  GM_OP_TOKEN_LOGPROBS = 7    /* B = rows M, k = topk, cfg->vocab = V */
 } gm_op;
 
 /* Decoder shape: pre-norm RMSNorm / RoPE (rotate-half, angle pos * base^(-2i/d))
@@ -365,6 +369,133 @@ gm_status gm_mtp_reconstruct(const gm_model_config *cfg, const gm_mtp_weights *m
 gm_status gm_dca_loss(int N, int K, int V, int topk, const float *head_logits, const uint16_t *rec_logp,
                       const int32_t *rec_ids, const int32_t *n_accept, int vgm, float *loss, float *alpha,
                       float *grad, void *ws, size_t ws_bytes, void *stream);
+
+/* ---- Draft trees.
+ * A tree of up to 64 nodes per sequence takes the place of the draft chain (the
+ * method drafts a chain, Sec. 2.2; a tree verifies several continuations at once):
+ * node 0 is the pending token t_m, node i > 0 continues node parents[b][i] < i.
+ * Node i's K/V entry is written at slot m_b + i, rotated at position m_b + depth_i
+ * (gm_kv_append), node i attends to the committed positions, to its ancestors and
+ * to itself (gm_tree_attention), the target's tokens select one path from the root
+ * (gm_tree_accept), and the path's entries move to the slots behind the committed
+ * length (gm_tree_commit).  n_nodes [B] (may be NULL: all N) are the nodes each
+ * sequence has, 0..N (values outside are clamped); the rest is padding. */
+
+/* Append: keys and values of T new positions, rotated and written into one layer of
+ * the cache, and (optionally) their queries rotated.  Sequence b owns the rows
+ * row_start[b] .. row_start[b+1] - 1 (row_start [B+1], increasing; NULL: T / B rows
+ * each, T a multiple of B); its i-th row goes to slot seq_lens[b] + i and is rotated
+ * at position seq_lens[b] + offsets[row] (offsets [T]; NULL: seq_lens[b] + i), so a
+ * prompt is appended in one call and a draft tree with its nodes' depths as offsets
+ * (plus 1 in the MTP head's cache, whose slots are rotated one position on).
+ * Rows outside every sequence's range are left alone.  seq_lens is not changed.
+ * k and v are [T][n_kv_heads][head_dim], q [T][n_heads][head_dim] in the model dtype;
+ * a row's heads are consecutive and rows are *_stride elements apart (the column
+ * blocks of one projection can be given in place).  q_out [T][n_heads][head_dim] is
+ * contiguous; it may be q itself if q is contiguous, and must not overlap q otherwise.
+ * q and q_out may both be NULL.  With cfg->qk_norm, k (and q) pass a per-head RMSNorm
+ * with weights k_norm and q_norm [head_dim] before the rotation.  Rotation: pairs
+ * (c, c + head_dim / 2) by position * rope_base^(-2 c / head_dim), angles in float64.
+ * max_rows (host): an upper bound on every sequence's rows.
+ * Errors: GM_ERR_CAPACITY if max_ctx + max_rows > max_pages_per_seq * page_size;
+ * dev_err GM_DEVERR_PAGE for a block-table entry outside the pool (its rows' K/V are
+ * not written; q_out is). */
+gm_status gm_kv_append(const gm_model_config *cfg, const gm_kv_cache *cache, int layer, int B, int T, int max_rows,
+                       const int32_t *row_start, const int32_t *offsets, const void *q, int64_t q_stride,
+                       const void *k, int64_t k_stride, const void *v, int64_t v_stride, const void *q_norm,
+                       const void *k_norm, void *q_out, int32_t *dev_err, void *stream);
+
+/* The plan of a batch of trees, made once per step and read by every layer: masks
+ * [B][N], bit j of masks[b][i] set iff node j is i or an ancestor of i, and depths
+ * [B][N] (0 for node 0).  A node whose parent is outside -1 .. i-1, or not a node of
+ * the tree, has no ancestors (dev_err GM_DEVERR_TREE); parent -1 is allowed for any
+ * node (such a node continues the committed tokens, as node 0 does).  Nodes past
+ * n_nodes[b] get mask 0 and depth 0. */
+gm_status gm_tree_masks(int B, int N, const int32_t *parents, const int32_t *n_nodes, uint64_t *masks,
+                        int32_t *depths, int32_t *dev_err, void *stream);
+
+/* Attention of one layer over the cache for the nodes of a tree: node i of sequence b
+ * attends to positions 0 .. m_b - 1 and to m_b + j for every bit j < n_nodes[b] of
+ * masks[b][i] (any set of nodes: gm_tree_masks makes those of a tree; the entries must
+ * already be in the cache).  q and out are [B][N][n_heads][head_dim] in the model
+ * dtype, q after the rotation; scale 1 / sqrt(head_dim), query head h reads KV head
+ * h / (n_heads / n_kv_heads).  Rows of padding nodes, and of nodes that see nothing,
+ * are 0.  A node's row does not depend on entries it does not attend to, whatever
+ * they hold.
+ * Limits: 1 <= N <= 64, n_heads / n_kv_heads <= 64.
+ * Errors: GM_ERR_CAPACITY if max_ctx + N > max_pages_per_seq * page_size; dev_err
+ * GM_DEVERR_PAGE for a block-table entry outside the pool (its positions are not
+ * attended to; which of those behind them are is not specified). */
+gm_status gm_tree_attention(const gm_model_config *cfg, const gm_kv_cache *cache, int layer, int B, int N,
+                            const void *q, const uint64_t *masks, const int32_t *n_nodes, void *out, void *ws,
+                            size_t ws_bytes, int32_t *dev_err, void *stream);
+
+/* The accept of a tree.  next_ids [B][N] holds the target's own token after each node:
+ * its arg-max (greedy), or a draw from its distribution at that node (each node's
+ * draw an independent one: the committed tokens are then distributed as the target's,
+ * whatever the tree holds).  From node 0 the walk goes on to the child whose token is
+ * next_ids of the node it stands on (the lowest index if several), until there is none.
+ * Outputs: n_accept [B], the accepted nodes without node 0; path [B][N] = 0, the
+ * accepted nodes in order, -1 pad; out_tokens [B][N] = the accepted nodes' tokens, then
+ * next_ids of the last node, -1 pad.  A sequence with n_nodes[b] = 0 gets n_accept -1
+ * and -1 throughout. */
+gm_status gm_tree_accept(int B, int N, const int32_t *parents, const int32_t *tokens, const int32_t *next_ids,
+                         const int32_t *n_nodes, int32_t *path, int32_t *n_accept, int32_t *out_tokens, void *stream);
+
+/* Commit of a tree's path: in every layer of the cache the K and V entries of slot
+ * m_b + path[b][i] move to slot m_b + i, i = 0 .. n_accept[b], and seq_lens[b] grows by
+ * n_accept[b] + 1; the rest is rolled back by index only.  path is increasing with
+ * path[b][i] >= i, as gm_tree_accept writes it (a sequence's entries that are not are
+ * left where they are: dev_err GM_DEVERR_TREE); n_accept is clamped to -1 .. N-1.  The
+ * cache's page pools are those of cfg's dtype, n_kv_heads and head_dim; every layer of
+ * the cache is committed (n_layers need not be cfg's: the MTP head's cache has one).
+ * committed_slots [B][N] (may be NULL): the physical slot (page * page_size + offset)
+ * of each committed position, -1 for the others.  dev_err GM_DEVERR_PAGE for a
+ * block-table entry outside the pool (that entry does not move). */
+gm_status gm_tree_commit(const gm_model_config *cfg, const gm_kv_cache *cache, int B, int N, const int32_t *path,
+                         const int32_t *n_accept, int32_t *committed_slots, int32_t *dev_err, void *stream);
+
+/* Softmax statistics that gm_token_logprobs leaves for its gradient: the row's largest
+ * logit and sum over ids of exp((z - max) / T).  (log-sum-exp of z / T = max / T + log sum.) */
+typedef struct {
+  float max;
+  float sum;
+} gm_token_stats;
+
+/* Log-probabilities of given tokens under softmax(z / T), with the entropy and the most
+ * likely alternatives: the policy's side of an RL update, the target's choice at a
+ * tree's nodes, and the candidates a tree is grown from.
+ * logits [M][V], dtype GM_F32 or GM_BF16, rows ld elements apart (ld >= V).  Each output
+ * may be NULL:
+ *   logp [M]: log p(ids[m]), 0 where ids[m] < 0 (no token); needs ids [M].  An id >= V
+ *     counts as no token (dev_err GM_DEVERR_TOKEN).
+ *   entropy [M]: -sum p log p (ids of probability 0 add 0).
+ *   top_logp, top_ids [M][topk] (both or neither): the topk largest logits' log p and
+ *     ids, in decreasing logit, equal logits in increasing id; 1 <= topk <= min(64, V).
+ *   stats [M]: for gm_token_logprobs_grad.
+ * Sums are float32 over at most 64 ids and float64 beyond.  Logits of -inf have
+ * probability 0; a log p below float32's range is -inf.  A row without any other logit: log p -inf, entropy 0, stats (-inf, 0),
+ * alternatives 0 .. topk-1.  A row that holds NaN or +inf gives NaN log p and entropy,
+ * and alternatives -1.
+ * Limits: V <= 524288, M <= 2^23. */
+gm_status gm_token_logprobs(int M, int V, int dtype, const void *logits, int64_t ld, float temperature,
+                            const int32_t *ids, float *logp, float *entropy, int topk, float *top_logp,
+                            int32_t *top_ids, gm_token_stats *stats, void *ws, size_t ws_bytes, int32_t *dev_err,
+                            void *stream);
+
+/* Its gradient in the logits: grad[m][x] = g_logp[m] d logp[m] / d z_x
+ * + g_entropy[m] d entropy[m] / d z_x
+ *   = ([x = ids[m]] g_logp - p_x (g_logp + g_entropy (log p_x + entropy))) / T,
+ * with g_logp taken as 0 where ids[m] is no token.  logits, ld, ids and temperature as
+ * in the call that wrote stats (and entropy); g_entropy may be NULL (0), else entropy is
+ * needed; ids and g_logp may both be NULL.  grad [M][V] has the logits' dtype (rounded
+ * once, from float32) and rows ld_grad elements apart; it may be the logits themselves
+ * (with the same ld), and must not overlap them otherwise.  A row whose statistics are
+ * (-inf, 0) gets 0.  The alternatives have no gradient. */
+gm_status gm_token_logprobs_grad(int M, int V, int dtype, const void *logits, int64_t ld, float temperature,
+                                 const int32_t *ids, const gm_token_stats *stats, const float *entropy,
+                                 const float *g_logp, const float *g_entropy, void *grad, int64_t ld_grad,
+                                 void *stream);
 
 /* Thread-local message describing the last non-OK status of this thread. */
 const char *gm_last_error(void);

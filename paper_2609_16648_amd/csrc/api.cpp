@@ -2,6 +2,7 @@
 // Every entry point validates on the host, then enqueues on the caller's
 // stream and returns without synchronising.
 #include <stdarg.h>
+#include <math.h>
 #include <stddef.h>
 #include <stdio.h>
 
@@ -9,6 +10,7 @@
 
 #include "forward.h"
 #include "launch.h"
+#include "tree.h"
 
 using namespace gm;
 
@@ -125,8 +127,15 @@ gm_status check_ws(void *ws, size_t have, size_t need) {
 extern "C" const char *gm_last_error(void) { return g_err.c_str(); }
 
 extern "C" size_t gm_workspace_size(int op, const gm_model_config *cfg, int B, int k, int max_ctx) {
-  if (B < 0 || k < 0 || k > kMaxK || max_ctx < 0) return 0;
+  if (B < 0 || k < 0 || max_ctx < 0) return 0;
+  if (k > kMaxK && op != GM_OP_TREE_ATTENTION && op != GM_OP_TOKEN_LOGPROBS) return 0;
   switch (op) {
+    case GM_OP_TREE_ATTENTION:
+      if (k < 1 || k > kMaxNodes || check_config(cfg, B, 0) != GM_OK) return 0;
+      return plan_tree_attention(*cfg, B, k).total;
+    case GM_OP_TOKEN_LOGPROBS:
+      if (!cfg || B > kLpMaxRows || k > kLpMaxTopk || cfg->vocab < 1 || cfg->vocab > kMaxVocab) return 0;
+      return logprobs_workspace(B, cfg->vocab, k);
     case GM_OP_SPEC_ACCEPT:
       if (!cfg || cfg->vocab < 1) return 0;
       return plan_accept(B, k, cfg->vocab).total;
@@ -404,4 +413,182 @@ extern "C" gm_status gm_mtp_reconstruct(const gm_model_config *cfg, const gm_mtp
   run_mtp_reconstruct(*cfg, *mtp, *shared, *mtp_cache, R, K, start_hidden, start_tokens, drafts, head_logits, p,
                       (char *)ws, dev_err, (hipStream_t)stream);
   return check_launch("gm_mtp_reconstruct");
+}
+
+// ---------------------------------------------------------------- draft trees
+extern "C" gm_status gm_kv_append(const gm_model_config *cfg, const gm_kv_cache *cache, int layer, int B, int T,
+                                  int max_rows, const int32_t *row_start, const int32_t *offsets, const void *q,
+                                  int64_t q_stride, const void *k, int64_t k_stride, const void *v, int64_t v_stride,
+                                  const void *q_norm, const void *k_norm, void *q_out, int32_t *dev_err,
+                                  void *stream) {
+  gm_status st = check_config(cfg, B, 0);
+  if (st != GM_OK) return st;
+  if (T < 0 || max_rows < 0 || max_rows > T) return fail(GM_ERR_INVALID_ARG, "bad T=%d max_rows=%d", T, max_rows);
+  if (T > kMaxAppendRows || B > kMaxTrees)
+    return fail(GM_ERR_UNSUPPORTED, "%d rows of %d sequences exceed %d of %d", T, B, kMaxAppendRows, kMaxTrees);
+  if (!cache) return fail(GM_ERR_INVALID_ARG, "null cache");
+  if (layer < 0 || layer >= cache->n_layers) return fail(GM_ERR_INVALID_ARG, "layer %d outside [0, %d)", layer, cache->n_layers);
+  st = check_cache(cfg, cache, cache->n_layers, max_rows, "gm_kv_append");
+  if (st != GM_OK) return st;
+  if (B == 0 || T == 0) return GM_OK;
+  if (!row_start && (T % B || max_rows < T / B))
+    return fail(GM_ERR_INVALID_ARG, "without row_start, T = %d is B = %d times at most max_rows = %d rows", T, B, max_rows);
+  if (!k || !v) return fail(GM_ERR_INVALID_ARG, "null k / v");
+  if (!q != !q_out) return fail(GM_ERR_INVALID_ARG, "q and q_out go together");
+  const int64_t kw = (int64_t)cfg->n_kv_heads * cfg->head_dim, qw = (int64_t)cfg->n_heads * cfg->head_dim;
+  if (k_stride < kw || v_stride < kw || (q && q_stride < qw))
+    return fail(GM_ERR_INVALID_ARG, "row strides %lld, %lld, %lld are less than a row", (long long)q_stride,
+                (long long)k_stride, (long long)v_stride);
+  if (cfg->qk_norm && (!k_norm || (q && !q_norm))) return fail(GM_ERR_INVALID_ARG, "qk_norm set but q_norm/k_norm null");
+  AppendArgs a{};
+  a.dtype = cfg->dtype;
+  a.B = B;
+  a.T = T;
+  a.n_heads = q ? cfg->n_heads : 0;
+  a.n_kv = cfg->n_kv_heads;
+  a.head_dim = cfg->head_dim;
+  a.page_size = cache->page_size;
+  a.max_pages = cache->max_pages_per_seq;
+  a.num_pages = cache->num_pages;
+  a.row_start = row_start;
+  a.offsets = offsets;
+  a.block_table = cache->block_table;
+  a.seq_lens = cache->seq_lens;
+  a.q = q;
+  a.k = k;
+  a.v = v;
+  a.q_stride = q_stride;
+  a.k_stride = k_stride;
+  a.v_stride = v_stride;
+  a.q_norm = cfg->qk_norm ? q_norm : nullptr;
+  a.k_norm = cfg->qk_norm ? k_norm : nullptr;
+  a.q_out = q_out;
+  a.k_pages = cache->k_pages[layer];
+  a.v_pages = cache->v_pages[layer];
+  a.log2_base = log2((double)cfg->rope_base);
+  a.eps = cfg->rms_eps;
+  a.dev_err = dev_err;
+  launch_kv_append(a, (hipStream_t)stream);
+  return check_launch("gm_kv_append");
+}
+
+namespace {
+gm_status check_tree(int B, int N) {
+  if (B < 0) return fail(GM_ERR_INVALID_ARG, "B = %d < 0", B);
+  if (B > kMaxTrees) return fail(GM_ERR_UNSUPPORTED, "%d trees exceed %d", B, kMaxTrees);
+  if (N < 1 || N > kMaxNodes) return fail(GM_ERR_UNSUPPORTED, "N = %d nodes outside [1, %d]", N, kMaxNodes);
+  return GM_OK;
+}
+}  // namespace
+
+extern "C" gm_status gm_tree_masks(int B, int N, const int32_t *parents, const int32_t *n_nodes, uint64_t *masks,
+                                   int32_t *depths, int32_t *dev_err, void *stream) {
+  gm_status st = check_tree(B, N);
+  if (st != GM_OK) return st;
+  if (B == 0) return GM_OK;
+  if (!parents || !masks || !depths) return fail(GM_ERR_INVALID_ARG, "null parents / masks / depths");
+  launch_tree_masks(B, N, parents, n_nodes, masks, depths, dev_err, (hipStream_t)stream);
+  return check_launch("gm_tree_masks");
+}
+
+extern "C" gm_status gm_tree_attention(const gm_model_config *cfg, const gm_kv_cache *cache, int layer, int B, int N,
+                                       const void *q, const uint64_t *masks, const int32_t *n_nodes, void *out,
+                                       void *ws, size_t ws_bytes, int32_t *dev_err, void *stream) {
+  gm_status st = check_config(cfg, B, 0);
+  if (st != GM_OK || (st = check_tree(B, N)) != GM_OK) return st;
+  if (!cache) return fail(GM_ERR_INVALID_ARG, "null cache");
+  if (layer < 0 || layer >= cache->n_layers) return fail(GM_ERR_INVALID_ARG, "layer %d outside [0, %d)", layer, cache->n_layers);
+  st = check_cache(cfg, cache, cache->n_layers, N, "gm_tree_attention");
+  if (st != GM_OK) return st;
+  if (B == 0) return GM_OK;
+  if (!q || !out || !masks) return fail(GM_ERR_INVALID_ARG, "null q / out / masks");
+  const AttnPlan p = plan_tree_attention(*cfg, B, N);
+  st = check_ws(ws, ws_bytes, p.total);
+  if (st != GM_OK) return st;
+  AttnArgs a = attn_args(*cfg, *cache, layer, B, N, cache->seq_lens, 0, n_nodes);
+  a.trace = "attn_tree";
+  a.trace_combine = "attn_tree_combine";
+  a.q = q;
+  a.out = out;
+  a.dev_err = dev_err;
+  run_tree_attention(a, masks, p, (char *)ws, (hipStream_t)stream);
+  return check_launch("gm_tree_attention");
+}
+
+extern "C" gm_status gm_tree_accept(int B, int N, const int32_t *parents, const int32_t *tokens,
+                                    const int32_t *next_ids, const int32_t *n_nodes, int32_t *path, int32_t *n_accept,
+                                    int32_t *out_tokens, void *stream) {
+  gm_status st = check_tree(B, N);
+  if (st != GM_OK) return st;
+  if (B == 0) return GM_OK;
+  if (!parents || !tokens || !next_ids) return fail(GM_ERR_INVALID_ARG, "null parents / tokens / next_ids");
+  if (!path || !n_accept || !out_tokens) return fail(GM_ERR_INVALID_ARG, "null path / n_accept / out_tokens");
+  launch_tree_accept(B, N, parents, tokens, next_ids, n_nodes, path, n_accept, out_tokens, (hipStream_t)stream);
+  return check_launch("gm_tree_accept");
+}
+
+extern "C" gm_status gm_tree_commit(const gm_model_config *cfg, const gm_kv_cache *cache, int B, int N,
+                                    const int32_t *path, const int32_t *n_accept, int32_t *committed_slots,
+                                    int32_t *dev_err, void *stream) {
+  gm_status st = check_config(cfg, B, 0);
+  if (st != GM_OK || (st = check_tree(B, N)) != GM_OK) return st;
+  if (!cache) return fail(GM_ERR_INVALID_ARG, "null cache");
+  if (cache->n_layers < 1) return fail(GM_ERR_INVALID_ARG, "cache without layers");
+  st = check_cache(cfg, cache, cache->n_layers, N, "gm_tree_commit");
+  if (st != GM_OK) return st;
+  if (B == 0) return GM_OK;
+  if (!path || !n_accept) return fail(GM_ERR_INVALID_ARG, "null path / n_accept");
+  launch_tree_commit(*cfg, *cache, B, N, path, n_accept, committed_slots, dev_err, (hipStream_t)stream);
+  return check_launch("gm_tree_commit");
+}
+
+// ---------------------------------------------------------------- token log-probabilities
+namespace {
+gm_status check_rows(int M, int V, int dtype, int64_t ld, float temperature) {
+  if (M < 0 || V < 1) return fail(GM_ERR_INVALID_ARG, "bad M=%d V=%d", M, V);
+  if (V > kMaxVocab) return fail(GM_ERR_UNSUPPORTED, "vocab %d exceeds %d", V, kMaxVocab);
+  if (M > kLpMaxRows) return fail(GM_ERR_UNSUPPORTED, "%d rows exceed %d", M, kLpMaxRows);
+  if (dtype != GM_F32 && dtype != GM_BF16) return fail(GM_ERR_INVALID_ARG, "unknown dtype %d", dtype);
+  if (ld < V) return fail(GM_ERR_INVALID_ARG, "rows of %d logits are %lld apart", V, (long long)ld);
+  if (!(temperature > 0.f) || !isfinite(temperature)) return fail(GM_ERR_INVALID_ARG, "temperature must be > 0 and finite");
+  return GM_OK;
+}
+}  // namespace
+
+extern "C" gm_status gm_token_logprobs(int M, int V, int dtype, const void *logits, int64_t ld, float temperature,
+                                       const int32_t *ids, float *logp, float *entropy, int topk, float *top_logp,
+                                       int32_t *top_ids, gm_token_stats *stats, void *ws, size_t ws_bytes,
+                                       int32_t *dev_err, void *stream) {
+  gm_status st = check_rows(M, V, dtype, ld, temperature);
+  if (st != GM_OK) return st;
+  if (!top_logp != !top_ids) return fail(GM_ERR_INVALID_ARG, "top_logp and top_ids go together");
+  if (top_ids && (topk < 1 || topk > kLpMaxTopk || topk > V))
+    return fail(GM_ERR_INVALID_ARG, "topk %d outside 1..min(%d, V)", topk, kLpMaxTopk);
+  if (M == 0) return GM_OK;
+  if (!logits) return fail(GM_ERR_INVALID_ARG, "null logits");
+  if (logp && !ids) return fail(GM_ERR_INVALID_ARG, "logp needs ids");
+  if (!logp && !entropy && !top_ids && !stats) return fail(GM_ERR_INVALID_ARG, "no output asked for");
+  if (!top_ids) topk = 0;
+  st = check_ws(ws, ws_bytes, logprobs_workspace(M, V, topk));
+  if (st != GM_OK) return st;
+  const LpOut o{ids, logp, entropy, top_logp, top_ids, stats, dev_err};
+  launch_token_logprobs(M, V, dtype, logits, ld, temperature, topk, o, (char *)ws, (hipStream_t)stream);
+  return check_launch("gm_token_logprobs");
+}
+
+extern "C" gm_status gm_token_logprobs_grad(int M, int V, int dtype, const void *logits, int64_t ld, float temperature,
+                                            const int32_t *ids, const gm_token_stats *stats, const float *entropy,
+                                            const float *g_logp, const float *g_entropy, void *grad, int64_t ld_grad,
+                                            void *stream) {
+  gm_status st = check_rows(M, V, dtype, ld, temperature);
+  if (st != GM_OK) return st;
+  if (ld_grad < V) return fail(GM_ERR_INVALID_ARG, "rows of %d gradients are %lld apart", V, (long long)ld_grad);
+  if (!ids != !g_logp) return fail(GM_ERR_INVALID_ARG, "ids and g_logp go together");
+  if (M == 0) return GM_OK;
+  if (!logits || !stats || !grad) return fail(GM_ERR_INVALID_ARG, "null logits / stats / grad");
+  if (g_entropy && !entropy) return fail(GM_ERR_INVALID_ARG, "g_entropy needs entropy");
+  if (grad == logits && ld_grad != ld) return fail(GM_ERR_INVALID_ARG, "a gradient in place has the logits' row stride");
+  launch_token_logprobs_grad(M, V, dtype, logits, ld, temperature, ids, stats, entropy, g_logp, g_entropy, grad,
+                             ld_grad, (hipStream_t)stream);
+  return check_launch("gm_token_logprobs_grad");
 }

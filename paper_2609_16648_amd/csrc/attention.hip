@@ -30,7 +30,7 @@
 #include <atomic>
 
 #include "common.h"
-#include "forward.h"
+#include "tree.h"
 
 namespace gm {
 
@@ -65,6 +65,9 @@ struct AttnK {
   int B, base_off, blen_add, R, G, n_heads, n_kv, page_size, max_pages, num_pages, rows_pad;
   int parts, heads_per_group, row_tiles, waves_per_head;
   float scale_log2;
+  // draft trees: R of the N nodes of every sequence from node0 on, with their masks [B][N]
+  const unsigned long long *masks;
+  int N, node0;
 };
 
 __device__ __forceinline__ int block_rows(const int32_t *blen, int add, int b, int R) {
@@ -74,9 +77,10 @@ __device__ __forceinline__ int block_rows(const int32_t *blen, int add, int b, i
 }
 
 // 16-token tiles of sequence b: its context is its block's start m0 plus its valid block rows
+template <bool TREE>
 __device__ __forceinline__ int seq_tiles(const AttnK &a, int b, int &m0, int &rows) {
   m0 = a.base[b] + a.base_off;
-  rows = block_rows(a.blen, a.blen_add, b, a.R);
+  rows = block_rows(a.blen, a.blen_add, b, TREE ? a.N : a.R);
   const int L = m0 + rows;
   return L > 0 ? (L + 15) >> 4 : 0;
 }
@@ -113,6 +117,13 @@ __device__ __forceinline__ int block_excl_scan(int v, int *sh, int *total) {
 
 __device__ __forceinline__ uint32_t zero_half(uint32_t v, int hi) { return hi ? (v & 0x0000ffffu) : (v & 0xffff0000u); }
 
+// two bf16: those that are inf or NaN become 0
+__device__ __forceinline__ uint32_t finite_or_0(uint32_t v) {
+  if ((v & 0x7f80u) == 0x7f80u) v &= 0xffff0000u;
+  if ((v & 0x7f800000u) == 0x7f800000u) v &= 0x0000ffffu;
+  return v;
+}
+
 typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
 typedef float floatx2_t __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {   // round to nearest even
@@ -136,10 +147,19 @@ struct TileBuf {
 // for every query tile before the next, so the tiles' dependency chains interleave and
 // the V operands of P V are formed once for all of them; each tile's arithmetic is the
 // same as on its own.
-template <bool MASK, int RT>
+// TREE: `vis` is the block's start m0 for every row, and the token m0 + d is seen iff bit d of the row's
+// `anc` is set; a V that is not finite is kept from the rows that do not see its token (0 * inf is NaN).
+template <bool MASK, int RT, bool TREE>
 __device__ __forceinline__ void attn_tiles(int tb, int L, int g, float scale_log2, TileBuf &t,
-                                           const bf16x8_t (&qf)[RT][4], const int (&vis)[RT], float (&m)[RT],
+                                           const bf16x8_t (&qf)[RT][4], const int (&vis)[RT],
+                                           const unsigned long long (&anc)[RT], const uint16_t *vtile, float (&m)[RT],
                                            float (&l)[RT], floatx4_t (&O)[RT][8]) {
+  auto seen = [&](int u, int tok) {
+    if (!TREE) return tok < vis[u];
+    const int d = tok - vis[u];
+    return d < 0 || (d < kMaxNodes && (anc[u] >> d & 1));
+  };
+  bool wild = false;     // TREE: some V of the tile is inf or NaN
   if (MASK) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
@@ -149,6 +169,26 @@ __device__ __forceinline__ void attn_tiles(int tb, int L, int g, float scale_log
           if (e < 2) { t.v[p].x = zero_half(t.v[p].x, e); t.v[p].z = zero_half(t.v[p].z, e); }
           else { t.v[p].y = zero_half(t.v[p].y, e - 2); t.v[p].w = zero_half(t.v[p].w, e - 2); }
         }
+      }
+    }
+  }
+  if (MASK && TREE) {
+    bool mine = false;
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+      const uint32_t q[4] = {t.v[p].x, t.v[p].y, t.v[p].z, t.v[p].w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        mine = mine || (q[e] & 0x7f80u) == 0x7f80u || (q[e] & 0x7f800000u) == 0x7f800000u;
+    }
+    wild = __any(mine);
+    if (wild) {
+#pragma unroll
+      for (int p = 0; p < 4; ++p) {
+        t.v[p].x = finite_or_0(t.v[p].x);
+        t.v[p].y = finite_or_0(t.v[p].y);
+        t.v[p].z = finite_or_0(t.v[p].z);
+        t.v[p].w = finite_or_0(t.v[p].w);
       }
     }
   }
@@ -166,7 +206,7 @@ __device__ __forceinline__ void attn_tiles(int tb, int L, int g, float scale_log
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       s[u][r] = S[u][r] * scale_log2;
-      if (MASK && tb + 4 * g + r >= vis[u]) s[u][r] = -INFINITY;
+      if (MASK && !seen(u, tb + 4 * g + r)) s[u][r] = -INFINITY;
     }
     tmax[u] = fmaxf(fmaxf(s[u][0], s[u][1]), fmaxf(s[u][2], s[u][3]));
   }
@@ -212,6 +252,30 @@ __device__ __forceinline__ void attn_tiles(int tb, int L, int g, float scale_log
 #pragma unroll
     for (int u = 0; u < RT; ++u) O[u][mm] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(va), pb[u], O[u][mm], 0, 0, 0);
   }
+  if (MASK && TREE && wild) {
+    // the V left out above, added for the rows that see it: token by token, weight from the lane that holds it
+    const int j = threadIdx.x & 15;
+#pragma unroll
+    for (int u = 0; u < RT; ++u) {
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const float p = s[u][r] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s[u][r] - m[u]);
+#pragma unroll 1
+        for (int gt = 0; gt < 4; ++gt) {
+          const int tok = 4 * gt + r;
+          const float pt = __shfl(p, gt * 16 + j, kWave);
+          if (tb + tok >= L || !seen(u, tb + tok)) continue;
+#pragma unroll
+          for (int mm = 0; mm < 8; ++mm)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float v = bf16_to_f32(vtile[v_tile_off(tok, 16 * mm + 4 * g + e)]);
+              if (!(fabsf(v) < INFINITY)) O[u][mm][e] += pt * v;
+            }
+        }
+      }
+    }
+  }
 }
 
 // RT: 16-row query tiles per wave.  A wave streams the KV tiles of its head once and
@@ -221,7 +285,8 @@ __device__ __forceinline__ void attn_tiles(int tb, int L, int g, float scale_log
 // marked non-temporal and do not displace the lines other waves re-read; where two waves
 // read the same tiles the second read is meant to hit the cache (measured: non-temporal
 // loads there cost 20%).
-template <bool STREAM, int RT>
+// TREE: the rows are nodes node0 .. node0 + R - 1 of each sequence's N (their masks in place of the causal window).
+template <bool STREAM, int RT, bool TREE>
 __global__ __launch_bounds__(64 * kAttnWavesPerGroup) void attn_mfma_kernel(AttnK a) {
   const int part = blockIdx.x, grp = blockIdx.y;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);   // wave index, uniform per wave
@@ -244,12 +309,12 @@ __global__ __launch_bounds__(64 * kAttnWavesPerGroup) void attn_mfma_kernel(Attn
   const bool writer = part == 0 && grp == 0;
   int TT = 0, T1 = 0, cb1 = 0, m1 = 0, r1 = 0;   // this thread's sequence of the chunk
   if (one_chunk) {
-    T1 = tid < a.B ? seq_tiles(a, tid, m1, r1) : 0;
+    T1 = tid < a.B ? seq_tiles<TREE>(a, tid, m1, r1) : 0;
     cb1 = block_excl_scan(T1, scan_sh, &TT);
     if (writer && tid < a.B) a.cum[tid] = cb1;
   } else {
     for (int c = 0; c < a.B; c += nthr) {
-      const int T = c + tid < a.B ? seq_tiles(a, c + tid, m1, r1) : 0;
+      const int T = c + tid < a.B ? seq_tiles<TREE>(a, c + tid, m1, r1) : 0;
       int tot;
       const int cb = TT + block_excl_scan(T, scan_sh, &tot);
       if (writer && c + tid < a.B) a.cum[c + tid] = cb;
@@ -270,8 +335,16 @@ __global__ __launch_bounds__(64 * kAttnWavesPerGroup) void attn_mfma_kernel(Attn
     qi[u] = r < rows && wave_ok ? r % a.R : -1;
     qrow[u] = qi[u] >= 0 ? (qi[u] * a.n_heads + kvh * a.G + r / a.R) * 128 + 8 * g : 0;
   }
+  // rows of a sequence in q and out, and the first of this launch's
+  const int q_rows = TREE ? a.N : a.R, q_row0 = TREE ? a.node0 : 0;
+  unsigned long long anc[RT], ancn[RT];
   auto load_q = [&](int b, bf16x8_t (&q)[RT][4]) {
-    const uint16_t *qb = a.q + (long)b * a.R * a.n_heads * 128;
+    const uint16_t *qb = a.q + ((long)b * q_rows + q_row0) * a.n_heads * 128;
+    if (TREE) {
+#pragma unroll
+      for (int u = 0; u < RT; ++u)
+        ancn[u] = qi[u] >= 0 ? a.masks[(long)b * a.N + a.node0 + qi[u]] : 0ull;
+    }
 #pragma unroll
     for (int u = 0; u < RT; ++u)
 #pragma unroll
@@ -322,7 +395,7 @@ __global__ __launch_bounds__(64 * kAttnWavesPerGroup) void attn_mfma_kernel(Attn
         continue;
       }
       // rows with no visible token (past the block, or none readable) give 0
-      const bool live = vis[u] > 0 && m[u] != -INFINITY;
+      const bool live = (TREE ? vis[u] >= 0 : vis[u] > 0) && m[u] != -INFINITY;
       const float inv = 1.f / lu;
       wave_lds_sync();
 #pragma unroll
@@ -340,7 +413,7 @@ __global__ __launch_bounds__(64 * kAttnWavesPerGroup) void attn_mfma_kernel(Attn
 #pragma unroll
         for (int c = 0; c < 4; ++c)
           pk[c] = f32_to_bf16(src[2 * c]) | (uint32_t(f32_to_bf16(src[2 * c + 1])) << 16);
-        const long o = (((long)b * a.R + r % a.R) * a.n_heads + kvh * a.G + r / a.R) * 128 + 8 * j;
+        const long o = (((long)b * q_rows + q_row0 + r % a.R) * a.n_heads + kvh * a.G + r / a.R) * 128 + 8 * j;
         *reinterpret_cast<uint4 *>(a.out + o) = make_uint4(pk[0], pk[1], pk[2], pk[3]);
       }
     }
@@ -354,7 +427,7 @@ __global__ __launch_bounds__(64 * kAttnWavesPerGroup) void attn_mfma_kernel(Attn
       cbt = cb1;
       tot = TT;
     } else {
-      T = c + tid < a.B ? seq_tiles(a, c + tid, m1, r1) : 0;
+      T = c + tid < a.B ? seq_tiles<TREE>(a, c + tid, m1, r1) : 0;
       cbt = run + block_excl_scan(T, scan_sh, &tot);
     }
     const int cbeg = run, cend = run + tot;
@@ -423,10 +496,24 @@ __global__ __launch_bounds__(64 * kAttnWavesPerGroup) void attn_mfma_kernel(Attn
           for (int u = 0; u < RT; ++u)
 #pragma unroll
             for (int ii = 0; ii < 4; ++ii) asm volatile("" : "+v"(qf[u][ii]));
+          if (TREE) {
+#pragma unroll
+            for (int u = 0; u < RT; ++u) {
+              anc[u] = ancn[u];
+              asm volatile("" : "+v"(anc[u]));
+            }
+          }
           if (seg_end < x0 + nt) load_q(c + __builtin_amdgcn_readfirstlane(seq_sh[seg_end - x0]), qn);
 #pragma unroll
           for (int u = 0; u < RT; ++u) {
-            vis[u] = qi[u] >= 0 && qi[u] < blen ? m0 + qi[u] + 1 : 0;
+            if (TREE) {
+              const bool node = qi[u] >= 0 && a.node0 + qi[u] < blen;
+              vis[u] = node ? m0 : -1;
+              if (!node) anc[u] = 0;
+              else if (blen < kMaxNodes) anc[u] &= (1ull << blen) - 1;
+            } else {
+              vis[u] = qi[u] >= 0 && qi[u] < blen ? m0 + qi[u] + 1 : 0;
+            }
             m[u] = -INFINITY;
             l[u] = 0.f;
 #pragma unroll
@@ -440,8 +527,10 @@ __global__ __launch_bounds__(64 * kAttnWavesPerGroup) void attn_mfma_kernel(Attn
         // the context) take the mask, which zeroes the V entries past the context in place.  Rows
         // that are not valid queries (past the block, or padding) compute finite values nobody reads.
         const int tb = 16 * (x - cb);
-        if (tb + 16 <= m0 + 1) attn_tiles<false, RT>(tb, L, g, a.scale_log2, t, qf, vis, m, l, O);
-        else attn_tiles<true, RT>(tb, L, g, a.scale_log2, t, qf, vis, m, l, O);
+        // (A tree's nodes need not see position m0.)
+        const uint16_t *vt = a.vp + head_off + (long)t.slot * 2048;
+        if (tb + 16 <= m0 + (TREE ? 0 : 1)) attn_tiles<false, RT, TREE>(tb, L, g, a.scale_log2, t, qf, vis, anc, vt, m, l, O);
+        else attn_tiles<true, RT, TREE>(tb, L, g, a.scale_log2, t, qf, vis, anc, vt, m, l, O);
       };
       // The ring runs across segments: the loads of the next sequence's tiles are in flight while
       // this one's last tiles are consumed.  The loads run unguarded in whole turns of the ring
@@ -494,7 +583,7 @@ __global__ __launch_bounds__(64 * kAttnWavesPerGroup) void attn_mfma_kernel(Attn
 // load round trips (one sequence in 126 partials: 42 us with one group, 8.5 with sixteen).
 constexpr int kCombineBatch = 8;
 
-template <int SP>
+template <int SP, bool TREE>
 __global__ __launch_bounds__(SP > 1 ? 32 * SP : 256) void attn_combine_kernel(AttnK a) {
   const int b = blockIdx.y;
   const int rows = a.G * a.R;
@@ -502,7 +591,7 @@ __global__ __launch_bounds__(SP > 1 ? 32 * SP : 256) void attn_combine_kernel(At
   const int idx = SP > 1 ? blockIdx.x * 32 + (tid & 31) : blockIdx.x * blockDim.x + tid;
   if (idx >= a.n_kv * rows * 32) return;   // (SP > 1: a block per row, never taken)
   const int d = (idx & 31) * 4, r = (idx >> 5) % rows, kvh = (idx >> 5) / rows;
-  const int hl = r / a.R, i = r % a.R;
+  const int hl = r / a.R, i = (TREE ? a.node0 : 0) + r % a.R;
   const int TT = a.cum[a.B], cb = a.cum[b], T = a.cum[b + 1] - cb, P = a.parts;
   int pf = 0, pl = 0;
   if (T > 0) {
@@ -510,7 +599,7 @@ __global__ __launch_bounds__(SP > 1 ? 32 * SP : 256) void attn_combine_kernel(At
     pl = min(div_u((unsigned long long)(cb + T) * P - 1, TT), P - 1);
     if (pf == pl) return;   // wholly in range pf, which has written its rows
   }
-  const int blen = block_rows(a.blen, a.blen_add, b, a.R);
+  const int blen = block_rows(a.blen, a.blen_add, b, TREE ? a.N : a.R);
   float M = -INFINITY, den = 0.f;
   float4 num = make_float4(0.f, 0.f, 0.f, 0.f);
   auto merge = [&](float m2, float l2, float4 o2) {
@@ -567,7 +656,7 @@ __global__ __launch_bounds__(SP > 1 ? 32 * SP : 256) void attn_combine_kernel(At
   }
   const uint2 packed = make_uint2(f32_to_bf16(v.x) | (uint32_t(f32_to_bf16(v.y)) << 16),
                                   f32_to_bf16(v.z) | (uint32_t(f32_to_bf16(v.w)) << 16));
-  *reinterpret_cast<uint2 *>(a.out + (((long)b * a.R + i) * a.n_heads + kvh * a.G + hl) * 128 + d) = packed;
+  *reinterpret_cast<uint2 *>(a.out + (((long)b * (TREE ? a.N : a.R) + i) * a.n_heads + kvh * a.G + hl) * 128 + d) = packed;
 }
 
 // ------------------------------------------------------------------ float32 path
@@ -578,6 +667,7 @@ struct AttnF {
   int32_t *dev_err;
   int base_off, blen_add, R, G, n_heads, n_kv, page_size, max_pages, num_pages;
   float scale;
+  const unsigned long long *masks;   // draft trees: [B][R], in place of the causal window
 };
 
 // One workgroup of four waves per (block row, head, sequence).  A wave takes every fourth
@@ -588,7 +678,8 @@ struct AttnF {
 // Bound by the chain of dependent loads, not by bytes (16 rows x 4 heads of 128 tokens:
 // 18 us with one wave per row whose lanes each walked the channels of their own tokens,
 // 6.8 us here).
-template <int D>
+// TREE: the row is a node, whose mask says which of the block's tokens it sees; V of the others is taken as 0.
+template <int D, bool TREE>
 __global__ __launch_bounds__(256) void attn_f32_kernel(AttnF a) {
   constexpr int C = D / 64;        // channels per lane in P V
   __shared__ float sh_q[D];
@@ -602,7 +693,19 @@ __global__ __launch_bounds__(256) void attn_f32_kernel(AttnF a) {
     for (int c = tid; c < D; c += 256) orow[c] = 0.f;
     return;
   }
-  const int vis = a.base[b] + a.base_off + i + 1;
+  const int m0 = a.base[b] + a.base_off;
+  unsigned long long anc = 0;
+  int vis = m0 + i + 1;            // tokens up to the last one that is seen
+  if (TREE) {
+    anc = a.masks[(long)b * a.R + i];
+    if (blen < kMaxNodes) anc &= (1ull << blen) - 1;
+    vis = anc ? m0 + 64 - __clzll(anc) : m0;
+  }
+  auto seen = [&](int tok) {
+    if (!TREE) return tok < vis;
+    const int d = tok - m0;
+    return d < 0 || (d < kMaxNodes && (anc >> d & 1));
+  };
   const int kvh = h / a.G;
   for (int c = tid; c < D; c += 256) sh_q[c] = a.q[(((long)b * a.R + i) * a.n_heads + h) * D + c];
   __syncthreads();
@@ -619,7 +722,7 @@ __global__ __launch_bounds__(256) void attn_f32_kernel(AttnF a) {
   for (int c0 = 64 * w; c0 < vis; c0 += 256) {
     const int tok = c0 + lane;
     float sc = -INFINITY;
-    if (tok < vis) {
+    if (seen(tok)) {
       const long tile = tile_base(tok & ~15);
       if (tile < 0) {
         raise_dev_err(a.dev_err, GM_DEVERR_PAGE);
@@ -662,10 +765,10 @@ __global__ __launch_bounds__(256) void attn_f32_kernel(AttnF a) {
         for (int c = 0; c < C; ++c) {
           const floatx4u_t v = *reinterpret_cast<const floatx4u_t *>(a.vp + tile + v_tile_off(s, lane + 64 * c));
           // slots past the visible tokens may hold anything
-          o[c] += pv.x * (tb + s < vis ? v[0] : 0.f);
-          o[c] += pv.y * (tb + s + 1 < vis ? v[1] : 0.f);
-          o[c] += pv.z * (tb + s + 2 < vis ? v[2] : 0.f);
-          o[c] += pv.w * (tb + s + 3 < vis ? v[3] : 0.f);
+          o[c] += pv.x * (seen(tb + s) ? v[0] : 0.f);
+          o[c] += pv.y * (seen(tb + s + 1) ? v[1] : 0.f);
+          o[c] += pv.z * (seen(tb + s + 2) ? v[2] : 0.f);
+          o[c] += pv.w * (seen(tb + s + 3) ? v[3] : 0.f);
         }
       }
     }
@@ -689,7 +792,7 @@ __global__ __launch_bounds__(256) void attn_f32_kernel(AttnF a) {
       den += sh_l[u] * f;
       num += sh_o[u][tid] * f;
     }
-    orow[tid] = num / den;
+    orow[tid] = TREE && den == 0.f ? 0.f : num / den;   // (a node may see nothing)
   }
 }
 
@@ -721,12 +824,13 @@ int resident_groups(int block) {
   int v = cache[dev][wv].load();
   if (v > 0) return v;
   int per_cu = 0, cus = 0;
-  const void *kernels[] = {(const void *)attn_mfma_kernel<true, 1>, (const void *)attn_mfma_kernel<true, 2>,
-                           (const void *)attn_mfma_kernel<false, 2>};
+  const void *kernels[] = {(const void *)attn_mfma_kernel<true, 1, false>, (const void *)attn_mfma_kernel<true, 2, false>,
+                           (const void *)attn_mfma_kernel<false, 2, false>, (const void *)attn_mfma_kernel<true, 1, true>,
+                           (const void *)attn_mfma_kernel<true, 2, true>, (const void *)attn_mfma_kernel<false, 2, true>};
   bool ok = true;
   for (const void *f : kernels)
     ok = ok && hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, kAttnLdsReserve) == hipSuccess;
-  if (!ok || hipOccupancyMaxActiveBlocksPerMultiprocessor(&per_cu, attn_mfma_kernel<true, 2>, block, kAttnLdsReserve) != hipSuccess ||
+  if (!ok || hipOccupancyMaxActiveBlocksPerMultiprocessor(&per_cu, attn_mfma_kernel<true, 2, false>, block, kAttnLdsReserve) != hipSuccess ||
       hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || per_cu < 1 || cus < 1) {
     (void)hipGetLastError();
     return 256;
@@ -787,86 +891,135 @@ AttnArgs attn_args(const gm_model_config &cfg, const gm_kv_cache &c, int layer, 
   return a;
 }
 
+namespace {
+AttnK attn_k(const AttnArgs &a, const AttnPlan &p, const AttnGeom &geo, char *ws) {
+  AttnK k{};
+  k.kp = (const uint16_t *)a.k_pages;
+  k.vp = (const uint16_t *)a.v_pages;
+  k.bt = a.block_table;
+  k.base = a.base_lens;
+  k.blen = a.blk_len;
+  k.q = (const uint16_t *)a.q;
+  k.out = (uint16_t *)a.out;
+  k.part_o = (float *)(ws + p.part_o);
+  k.part_ml = (float2 *)(ws + p.part_ml);
+  k.cum = (int32_t *)(ws + p.cum);
+  k.dev_err = a.dev_err;
+  k.B = a.B;
+  k.base_off = a.base_off;
+  k.blen_add = a.blk_len_add;
+  k.R = a.R;
+  k.G = a.n_heads / a.n_kv;
+  k.n_heads = a.n_heads;
+  k.n_kv = a.n_kv;
+  k.page_size = a.page_size;
+  k.max_pages = a.max_pages;
+  k.num_pages = a.num_pages;
+  k.rows_pad = p.rows_pad;
+  k.parts = p.parts;
+  k.heads_per_group = geo.heads_per_group;
+  k.row_tiles = geo.row_tiles;
+  k.waves_per_head = geo.waves_per_head;
+  k.scale_log2 = a.scale * 1.4426950408889634f;
+  return k;
+}
+
+template <bool TREE>
+void launch_attn_mfma(const AttnK &k, const AttnGeom &geo, const char *trace, const char *trace_combine,
+                      hipStream_t s) {
+  {
+    TraceScope ts(trace, s);
+    const dim3 grid(k.parts, geo.groups), block(geo.block);
+    if (geo.rt_per_wave == 1)
+      hipLaunchKernelGGL((attn_mfma_kernel<true, 1, TREE>), grid, block, kAttnLdsReserve, s, k);
+    else if (geo.waves_per_head == 1)
+      hipLaunchKernelGGL((attn_mfma_kernel<true, 2, TREE>), grid, block, kAttnLdsReserve, s, k);
+    else
+      hipLaunchKernelGGL((attn_mfma_kernel<false, 2, TREE>), grid, block, kAttnLdsReserve, s, k);
+  }
+  TraceScope ts(trace_combine, s);
+  const int out_rows = k.n_kv * k.G * k.R;
+  // Sixteen groups per row save a round trip per eight partials of a sequence and cost a workgroup per
+  // row: taken where a sequence has more than a batch of partials and the launch at most 32 rows per
+  // partial of a sequence.  (Rows, partials: attention and combine with one group -> sixteen, us.
+  // 512, 32: 20.0 -> 16.3; 672, 43: 27.1 -> 21.8; 800, 26: 44.1 -> 42.5; 1024, 32: 28.0 -> 26.9;
+  // 672, 18: 18.6 -> 18.8; 1024, 16: 18.6 -> 20.1; 1344, 18: 23.1 -> 26.4; 2048, 8: 21.0 -> 30.5.)
+  if (k.parts >= 8 * k.B && (long)out_rows * k.B * k.B <= 32L * k.parts)
+    hipLaunchKernelGGL((attn_combine_kernel<16, TREE>), dim3(out_rows, k.B), dim3(512), 0, s, k);
+  else
+    hipLaunchKernelGGL((attn_combine_kernel<1, TREE>), dim3((out_rows + 7) / 8, k.B), dim3(256), 0, s, k);
+}
+
+template <bool TREE>
+void launch_attn_f32(const AttnArgs &a, const uint64_t *masks, hipStream_t s) {
+  AttnF f{};
+  f.kp = (const float *)a.k_pages;
+  f.vp = (const float *)a.v_pages;
+  f.q = (const float *)a.q;
+  f.out = (float *)a.out;
+  f.bt = a.block_table;
+  f.base = a.base_lens;
+  f.blen = a.blk_len;
+  f.dev_err = a.dev_err;
+  f.base_off = a.base_off;
+  f.blen_add = a.blk_len_add;
+  f.R = a.R;
+  f.G = a.n_heads / a.n_kv;
+  f.n_heads = a.n_heads;
+  f.n_kv = a.n_kv;
+  f.page_size = a.page_size;
+  f.max_pages = a.max_pages;
+  f.num_pages = a.num_pages;
+  f.scale = a.scale;
+  f.masks = (const unsigned long long *)masks;
+  dim3 grid(a.R, a.n_heads, a.B);
+  TraceScope ts(a.trace, s);
+  if (a.head_dim == 64) hipLaunchKernelGGL((attn_f32_kernel<64, TREE>), grid, dim3(256), 0, s, f);
+  else hipLaunchKernelGGL((attn_f32_kernel<128, TREE>), grid, dim3(256), 0, s, f);
+}
+
+AttnGeom geom_of(int n_kv, const AttnPlan &p) {
+  gm_model_config cfg{};
+  cfg.n_kv_heads = n_kv;
+  return attn_geom(cfg, p.rows_pad);
+}
+}  // namespace
+
 void run_attention(const AttnArgs &a, const AttnPlan &p, char *ws, hipStream_t s) {
   if (a.B == 0) return;
-  const int G = a.n_heads / a.n_kv;
   if (a.dtype == GM_BF16) {
-    gm_model_config cfg{};
-    cfg.n_kv_heads = a.n_kv;
-    const AttnGeom geo = attn_geom(cfg, p.rows_pad);
-    AttnK k{};
-    k.kp = (const uint16_t *)a.k_pages;
-    k.vp = (const uint16_t *)a.v_pages;
-    k.bt = a.block_table;
-    k.base = a.base_lens;
-    k.blen = a.blk_len;
-    k.q = (const uint16_t *)a.q;
-    k.out = (uint16_t *)a.out;
-    k.part_o = (float *)(ws + p.part_o);
-    k.part_ml = (float2 *)(ws + p.part_ml);
-    k.cum = (int32_t *)(ws + p.cum);
-    k.dev_err = a.dev_err;
-    k.B = a.B;
-    k.base_off = a.base_off;
-    k.blen_add = a.blk_len_add;
-    k.R = a.R;
-    k.G = G;
-    k.n_heads = a.n_heads;
-    k.n_kv = a.n_kv;
-    k.page_size = a.page_size;
-    k.max_pages = a.max_pages;
-    k.num_pages = a.num_pages;
-    k.rows_pad = p.rows_pad;
-    k.parts = p.parts;
-    k.heads_per_group = geo.heads_per_group;
-    k.row_tiles = geo.row_tiles;
-    k.waves_per_head = geo.waves_per_head;
-    k.scale_log2 = a.scale * 1.4426950408889634f;
-    {
-      TraceScope ts(a.trace, s);
-      const dim3 grid(p.parts, geo.groups), block(geo.block);
-      if (geo.rt_per_wave == 1)
-        hipLaunchKernelGGL((attn_mfma_kernel<true, 1>), grid, block, kAttnLdsReserve, s, k);
-      else if (geo.waves_per_head == 1)
-        hipLaunchKernelGGL((attn_mfma_kernel<true, 2>), grid, block, kAttnLdsReserve, s, k);
-      else
-        hipLaunchKernelGGL((attn_mfma_kernel<false, 2>), grid, block, kAttnLdsReserve, s, k);
-    }
-    TraceScope ts(a.trace_combine, s);
-    const int out_rows = a.n_kv * G * a.R;
-    // Sixteen groups per row save a round trip per eight partials of a sequence and cost a workgroup per
-    // row: taken where a sequence has more than a batch of partials and the launch at most 32 rows per
-    // partial of a sequence.  (Rows, partials: attention and combine with one group -> sixteen, us.
-    // 512, 32: 20.0 -> 16.3; 672, 43: 27.1 -> 21.8; 800, 26: 44.1 -> 42.5; 1024, 32: 28.0 -> 26.9;
-    // 672, 18: 18.6 -> 18.8; 1024, 16: 18.6 -> 20.1; 1344, 18: 23.1 -> 26.4; 2048, 8: 21.0 -> 30.5.)
-    if (p.parts >= 8 * a.B && (long)out_rows * a.B * a.B <= 32L * p.parts)
-      hipLaunchKernelGGL(attn_combine_kernel<16>, dim3(out_rows, a.B), dim3(512), 0, s, k);
-    else
-      hipLaunchKernelGGL(attn_combine_kernel<1>, dim3((out_rows + 7) / 8, a.B), dim3(256), 0, s, k);
+    const AttnGeom geo = geom_of(a.n_kv, p);
+    launch_attn_mfma<false>(attn_k(a, p, geo, ws), geo, a.trace, a.trace_combine, s);
   } else {
-    AttnF f{};
-    f.kp = (const float *)a.k_pages;
-    f.vp = (const float *)a.v_pages;
-    f.q = (const float *)a.q;
-    f.out = (float *)a.out;
-    f.bt = a.block_table;
-    f.base = a.base_lens;
-    f.blen = a.blk_len;
-    f.dev_err = a.dev_err;
-    f.base_off = a.base_off;
-    f.blen_add = a.blk_len_add;
-    f.R = a.R;
-    f.G = G;
-    f.n_heads = a.n_heads;
-    f.n_kv = a.n_kv;
-    f.page_size = a.page_size;
-    f.max_pages = a.max_pages;
-    f.num_pages = a.num_pages;
-    f.scale = a.scale;
-    dim3 grid(a.R, a.n_heads, a.B);
-    TraceScope ts(a.trace, s);
-    if (a.head_dim == 64) hipLaunchKernelGGL(attn_f32_kernel<64>, grid, dim3(256), 0, s, f);
-    else hipLaunchKernelGGL(attn_f32_kernel<128>, grid, dim3(256), 0, s, f);
+    launch_attn_f32<false>(a, nullptr, s);
+  }
+}
+
+// ---------------------------------------------------------------- draft trees
+// nodes of a sequence that one launch takes: as many as fill the rows of a KV head
+static int nodes_per_launch(int G, int N) {
+  const int n = kAttnMaxRows / G;
+  return n < N ? n : N;
+}
+
+AttnPlan plan_tree_attention(const gm_model_config &cfg, int B, int N) {
+  return plan_attention(cfg, B, nodes_per_launch(cfg.n_heads / cfg.n_kv_heads, N));
+}
+
+void run_tree_attention(const AttnArgs &a, const uint64_t *masks, const AttnPlan &p, char *ws, hipStream_t s) {
+  if (a.B == 0) return;
+  if (a.dtype != GM_BF16) {
+    launch_attn_f32<true>(a, masks, s);
+    return;
+  }
+  const AttnGeom geo = geom_of(a.n_kv, p);
+  AttnK k = attn_k(a, p, geo, ws);
+  k.masks = (const unsigned long long *)masks;
+  k.N = a.R;
+  const int step = nodes_per_launch(k.G, k.N);
+  for (k.node0 = 0; k.node0 < k.N; k.node0 += step) {
+    k.R = k.N - k.node0 < step ? k.N - k.node0 : step;
+    launch_attn_mfma<true>(k, geo, a.trace, a.trace_combine, s);
   }
 }
 

@@ -5,6 +5,8 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include "../../include/gm.h"
+
 namespace gm {
 
 // ---------------------------------------------------------------- tracing
@@ -157,6 +159,29 @@ void launch_nucleus(const char *name, int n_rows, int V, double inv_td, double t
 // nucleus false: every row of sel keeps every id (top-p 1), and the kernels skip the nucleus tests
 void launch_residual_draw(const char *chunk_name, const char *scan_name, int B, int V, float inv_t, const RowSel *sel,
                           double *wsum, double *psum, bool nucleus, hipStream_t s);
+
+// ---------------------------------------------------------------- token log-probabilities (logprob.hip)
+constexpr int kLpChunk = 16384;     // ids per workgroup of the forward pass
+constexpr int kLpMaxTopk = 64;
+constexpr int kLpMaxRows = 1 << 23; // rows per call: a workgroup each of 256 threads, less than 2^32 threads per launch
+inline int lp_chunks(int V) { return (V + kLpChunk - 1) / kLpChunk; }
+// Ids per run maximum of the alternatives' selection: at least 64 runs down to 512 ids, so that the runs'
+// maxima bound the 64th best logit, and at most 2048 of them, 32 per lane of a wave.
+inline int lp_run(int V) { return V > 16384 ? 256 : V > 2048 ? 32 : 8; }
+inline int lp_runs(int V) { return (V + lp_run(V) - 1) / lp_run(V); }
+struct LpOut {          // outputs of gm_token_logprobs; any may be null
+  const int32_t *ids;
+  float *logp, *entropy, *top_logp;
+  int32_t *top_ids;
+  gm_token_stats *stats;
+  int32_t *dev_err;
+};
+size_t logprobs_workspace(int M, int V, int topk);
+void launch_token_logprobs(int M, int V, int dtype, const void *logits, long ld, float temperature, int topk,
+                           const LpOut &o, char *ws, hipStream_t s);
+void launch_token_logprobs_grad(int M, int V, int dtype, const void *logits, long ld, float temperature,
+                                const int32_t *ids, const gm_token_stats *stats, const float *entropy,
+                                const float *g_logp, const float *g_entropy, void *grad, long ld_grad, hipStream_t s);
 
 // ---------------------------------------------------------------- KV index
 void launch_kv_commit(int B, int k, int page_size, int max_pages, const int32_t *block_table,

@@ -23,9 +23,10 @@ GM_OK, GM_ERR_INVALID_ARG, GM_ERR_UNSUPPORTED, GM_ERR_CAPACITY, GM_ERR_WORKSPACE
 GM_F32, GM_BF16 = 0, 1
 GM_GREEDY, GM_SAMPLE = 0, 1
 GM_OP_VERIFY_FORWARD, GM_OP_VERIFY_ATTENTION, GM_OP_SPEC_ACCEPT, GM_OP_MTP_DRAFT, GM_OP_DCA_LOSS = 0, 1, 2, 3, 4
-GM_OP_MTP_RECONSTRUCT = 5
-GM_DEVERR_TOKEN, GM_DEVERR_PAGE = 1, 2
+GM_OP_MTP_RECONSTRUCT, GM_OP_TREE_ATTENTION, GM_OP_TOKEN_LOGPROBS = 5, 6, 7
+GM_DEVERR_TOKEN, GM_DEVERR_PAGE, GM_DEVERR_TREE = 1, 2, 4
 
+c_int64 = ctypes.c_int64
 c_int, c_float, c_void_p, c_size_t, c_double = ctypes.c_int, ctypes.c_float, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_double
 
 
@@ -65,7 +66,9 @@ class KVCacheDesc(ctypes.Structure):
 _lib = None
 
 EXPORTS = ["gm_workspace_size", "gm_verify_forward", "gm_verify_attention", "gm_spec_accept", "gm_kv_commit",
-           "gm_mtp_draft", "gm_mtp_reconstruct", "gm_dca_loss", "gm_last_error", "gm_trace_every", "gm_trace_start", "gm_trace_stop", "gm_trace_count", "gm_trace_get", "gm_spec_accept_noalloc"]
+           "gm_mtp_draft", "gm_mtp_reconstruct", "gm_dca_loss", "gm_last_error", "gm_trace_every", "gm_trace_start", "gm_trace_stop", "gm_trace_count", "gm_trace_get", "gm_spec_accept_noalloc",
+           "gm_kv_append", "gm_tree_masks", "gm_tree_attention", "gm_tree_accept", "gm_tree_commit",
+           "gm_token_logprobs", "gm_token_logprobs_grad"]
 
 
 def lib() -> ctypes.CDLL:
@@ -105,6 +108,25 @@ def lib() -> ctypes.CDLL:
     L.gm_dca_loss.restype = c_int
     L.gm_dca_loss.argtypes = [c_int, c_int, c_int, c_int, c_void_p, c_void_p, c_void_p, c_void_p, c_int, c_void_p,
                               c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]
+    L.gm_kv_append.restype = c_int
+    L.gm_kv_append.argtypes = [P(ModelConfig), P(KVCacheDesc), c_int, c_int, c_int, c_int, c_void_p, c_void_p,
+                               c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_void_p, c_void_p,
+                               c_void_p, c_void_p]
+    L.gm_tree_masks.restype = c_int
+    L.gm_tree_masks.argtypes = [c_int, c_int] + [c_void_p] * 6
+    L.gm_tree_attention.restype = c_int
+    L.gm_tree_attention.argtypes = [P(ModelConfig), P(KVCacheDesc), c_int, c_int, c_int, c_void_p, c_void_p, c_void_p,
+                                    c_void_p, c_void_p, c_size_t, c_void_p, c_void_p]
+    L.gm_tree_accept.restype = c_int
+    L.gm_tree_accept.argtypes = [c_int, c_int] + [c_void_p] * 8
+    L.gm_tree_commit.restype = c_int
+    L.gm_tree_commit.argtypes = [P(ModelConfig), P(KVCacheDesc), c_int, c_int] + [c_void_p] * 5
+    L.gm_token_logprobs.restype = c_int
+    L.gm_token_logprobs.argtypes = [c_int, c_int, c_int, c_void_p, c_int64, c_float, c_void_p, c_void_p, c_void_p,
+                                    c_int, c_void_p, c_void_p, c_void_p, c_void_p, c_size_t, c_void_p, c_void_p]
+    L.gm_token_logprobs_grad.restype = c_int
+    L.gm_token_logprobs_grad.argtypes = [c_int, c_int, c_int, c_void_p, c_int64, c_float, c_void_p, c_void_p, c_void_p,
+                                         c_void_p, c_void_p, c_void_p, c_int64, c_void_p]
     L.gm_last_error.restype = ctypes.c_char_p
     L.gm_last_error.argtypes = []
     L.gm_trace_every.restype = c_int
@@ -234,11 +256,13 @@ class PagedCache:
 
     pages_needed[b] pages are dealt to sequence b from a shuffled pool, or the
     rows of an explicit page table (pages may then be shared between rows);
-    max_ctx is the host bound on the committed lengths."""
+    max_ctx is the host bound on the committed lengths.  pools: (k, v), each
+    [n_layers, num_pages, n_kv * page_size * head_dim], memory the caller holds
+    already, in place of new pools."""
 
     def __init__(self, shape, n_layers: int, lens: Sequence[int], capacity: Sequence[int], page_size: int = 16,
                  max_ctx: Optional[int] = None, device="cuda", seed: int = 0, fill: str = "zero",
-                 table: Optional[np.ndarray] = None):
+                 table: Optional[np.ndarray] = None, pools: Optional[Sequence[torch.Tensor]] = None):
         self.shape, self.n_layers, self.page_size = shape, n_layers, page_size
         self.dtype = torch_dtype(shape)
         lens = np.asarray(lens, dtype=np.int64)
@@ -258,9 +282,17 @@ class PagedCache:
         self.seq_lens = torch.from_numpy(lens.astype(np.int32)).to(device)
         self.max_ctx = int(lens.max()) if max_ctx is None else int(max_ctx)
         blk = shape.n_kv_heads * page_size * shape.head_dim
-        make = torch.zeros if fill == "zero" else torch.empty
-        self.k = [make((self.num_pages, blk), dtype=self.dtype, device=device) for _ in range(n_layers)]
-        self.v = [make((self.num_pages, blk), dtype=self.dtype, device=device) for _ in range(n_layers)]
+        if pools is not None:
+            pages = pools[0].shape[1] if pools[0].dim() == 3 else -1
+            for t, name in zip(pools, ("k pool", "v pool")):
+                _need(t, self.dtype, (n_layers, max(pages, self.num_pages), blk), name)
+                _ptr(t)
+            self.num_pages = pages
+            self.k, self.v = list(pools[0]), list(pools[1])
+        else:
+            make = torch.zeros if fill == "zero" else torch.empty
+            self.k = [make((self.num_pages, blk), dtype=self.dtype, device=device) for _ in range(n_layers)]
+            self.v = [make((self.num_pages, blk), dtype=self.dtype, device=device) for _ in range(n_layers)]
         self._kp = (c_void_p * n_layers)(*[t.data_ptr() for t in self.k])
         self._vp = (c_void_p * n_layers)(*[t.data_ptr() for t in self.v])
 
@@ -515,6 +547,170 @@ def dca_loss(head_logits: torch.Tensor, rec_logp: torch.Tensor, rec_ids: torch.T
     _check(lib().gm_dca_loss(N, K, V, topk, _ptr(head_logits), _ptr(rec_logp), _ptr(rec_ids), _ptr(n_accept),
                              int(bool(vgm)), _ptr(loss), _ptr(alpha), _ptr(grad), _ptr(buf), buf.numel(),
                              _stream(stream)))
+
+
+# ------------------------------------------------------------------------ draft trees
+def _rows(t: torch.Tensor, dtype, heads: int, dim: int, rows: int, name: str):
+    """A [rows, heads, dim] tensor whose rows may lie any distance apart: (pointer, row stride)."""
+    if t.dtype != dtype or t.shape != (rows, heads, dim):
+        raise ValueError("%s: expected %s %s, got %s %s" % (name, dtype, (rows, heads, dim), t.dtype, tuple(t.shape)))
+    if not t.is_cuda:
+        raise ValueError("%s must be a device tensor" % name)
+    if (dim > 1 and t.stride(2) != 1) or (heads > 1 and t.stride(1) != dim) or (rows > 1 and t.stride(0) < heads * dim):
+        raise ValueError("%s: the heads of a row must be contiguous and the rows apart" % name)
+    return c_void_p(t.data_ptr()), t.stride(0) if rows > 1 else heads * dim
+
+
+def kv_append(cfg: ModelConfig, cache: PagedCache, layer: int, k: torch.Tensor, v: torch.Tensor,
+              q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
+              row_start: Optional[torch.Tensor] = None, offsets: Optional[torch.Tensor] = None,
+              q_norm: Optional[torch.Tensor] = None, k_norm: Optional[torch.Tensor] = None,
+              max_rows: Optional[int] = None, dev_err: Optional[torch.Tensor] = None, stream=None):
+    """Keys and values [T, n_kv, head_dim] of new positions, rotated, into one layer of the cache, and
+    queries [T, n_heads, head_dim], rotated, into q_out (see gm.h).  Column blocks of one projection
+    can be passed as they are.  With row_start [B+1], max_rows (the most rows of a sequence) is
+    required; without it every sequence has T / B rows."""
+    T, B = k.shape[0], cache.B
+    dt, D = cache.dtype, cfg.head_dim
+    pk, sk = _rows(k, dt, cfg.n_kv_heads, D, T, "k")
+    pv, sv = _rows(v, dt, cfg.n_kv_heads, D, T, "v")
+    pq, sq = _rows(q, dt, cfg.n_heads, D, T, "q") if q is not None else (None, 0)
+    if q_out is not None:
+        _need(q_out, dt, (T, cfg.n_heads, D), "q_out")
+    if row_start is not None:
+        _need(row_start, torch.int32, (B + 1,), "row_start")
+        if max_rows is None:
+            raise ValueError("row_start needs max_rows")
+    elif max_rows is None:
+        max_rows = -(-T // B) if B else 0
+    if offsets is not None:
+        _need(offsets, torch.int32, (T,), "offsets")
+    for t, name in ((q_norm, "q_norm"), (k_norm, "k_norm")):
+        if t is not None:
+            _need(t, dt, (D,), name)
+    cs = cache.struct()
+    _check(lib().gm_kv_append(ctypes.byref(cfg), ctypes.byref(cs), layer, B, T, max_rows, _ptr(row_start),
+                              _ptr(offsets), pq, sq, pk, sk, pv, sv, _ptr(q_norm), _ptr(k_norm), _ptr(q_out),
+                              _ptr(dev_err), _stream(stream)))
+
+
+def tree_masks(parents: torch.Tensor, masks: torch.Tensor, depths: torch.Tensor,
+               n_nodes: Optional[torch.Tensor] = None, dev_err: Optional[torch.Tensor] = None, stream=None):
+    """Ancestor masks (int64 holding 64 bits) and depths of the trees parents [B, N] (see gm.h)."""
+    B, N = parents.shape
+    _need(parents, torch.int32, (B, N), "parents")
+    _need(masks, torch.int64, (B, N), "masks")
+    _need(depths, torch.int32, (B, N), "depths")
+    if n_nodes is not None:
+        _need(n_nodes, torch.int32, (B,), "n_nodes")
+    _check(lib().gm_tree_masks(B, N, _ptr(parents), _ptr(n_nodes), _ptr(masks), _ptr(depths), _ptr(dev_err),
+                               _stream(stream)))
+
+
+def tree_attention(cfg: ModelConfig, cache: PagedCache, layer: int, q: torch.Tensor, masks: torch.Tensor,
+                   out: torch.Tensor, ws: Workspace, n_nodes: Optional[torch.Tensor] = None,
+                   dev_err: Optional[torch.Tensor] = None, stream=None):
+    """Attention of the trees' nodes over the cache: node i sees the committed positions and the nodes of
+    masks[b, i] (see gm.h)."""
+    B, N = q.shape[0], q.shape[1]
+    _need(q, cache.dtype, (cache.B, N, cfg.n_heads, cfg.head_dim), "q")
+    _need(out, cache.dtype, (B, N, cfg.n_heads, cfg.head_dim), "out")
+    _need(masks, torch.int64, (B, N), "masks")
+    if n_nodes is not None:
+        _need(n_nodes, torch.int32, (B,), "n_nodes")
+    cs = cache.struct()
+    buf = ws.get(workspace_size(GM_OP_TREE_ATTENTION, cfg, B, N, cache.max_ctx))
+    _check(lib().gm_tree_attention(ctypes.byref(cfg), ctypes.byref(cs), layer, B, N, _ptr(q), _ptr(masks),
+                                   _ptr(n_nodes), _ptr(out), _ptr(buf), buf.numel(), _ptr(dev_err), _stream(stream)))
+
+
+def tree_accept(parents: torch.Tensor, tokens: torch.Tensor, next_ids: torch.Tensor, path: torch.Tensor,
+                n_accept: torch.Tensor, out_tokens: torch.Tensor, n_nodes: Optional[torch.Tensor] = None,
+                stream=None):
+    """The walk of each tree along the target's tokens next_ids [B, N] (see gm.h)."""
+    B, N = parents.shape
+    for t, name in ((parents, "parents"), (tokens, "tokens"), (next_ids, "next_ids"), (path, "path"),
+                    (out_tokens, "out_tokens")):
+        _need(t, torch.int32, (B, N), name)
+    _need(n_accept, torch.int32, (B,), "n_accept")
+    if n_nodes is not None:
+        _need(n_nodes, torch.int32, (B,), "n_nodes")
+    _check(lib().gm_tree_accept(B, N, _ptr(parents), _ptr(tokens), _ptr(next_ids), _ptr(n_nodes), _ptr(path),
+                                _ptr(n_accept), _ptr(out_tokens), _stream(stream)))
+
+
+def tree_commit(cfg: ModelConfig, cache: PagedCache, path: torch.Tensor, n_accept: torch.Tensor,
+                committed_slots: Optional[torch.Tensor] = None, dev_err: Optional[torch.Tensor] = None, stream=None):
+    """The accepted paths' entries behind the committed length in every layer of the cache (see gm.h)."""
+    B, N = path.shape
+    _need(path, torch.int32, (cache.B, N), "path")
+    _need(n_accept, torch.int32, (B,), "n_accept")
+    if committed_slots is not None:
+        _need(committed_slots, torch.int32, (B, N), "committed_slots")
+    cs = cache.struct()
+    _check(lib().gm_tree_commit(ctypes.byref(cfg), ctypes.byref(cs), B, N, _ptr(path), _ptr(n_accept),
+                                _ptr(committed_slots), _ptr(dev_err), _stream(stream)))
+
+
+# ------------------------------------------------------------------------ token log-probabilities
+def _logit_rows(t: torch.Tensor, name: str):
+    """A [M, V] float32 or bfloat16 tensor with contiguous rows: (pointer, gm dtype, row stride)."""
+    if t.dim() != 2 or t.dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError("%s: expected float32 or bfloat16 [M, V], got %s %s" % (name, t.dtype, tuple(t.shape)))
+    if not t.is_cuda:
+        raise ValueError("%s must be a device tensor" % name)
+    M, V = t.shape
+    if (V > 1 and t.stride(1) != 1) or (M > 1 and t.stride(0) < V):
+        raise ValueError("%s: the ids of a row must be contiguous and the rows apart" % name)
+    return c_void_p(t.data_ptr()), GM_BF16 if t.dtype == torch.bfloat16 else GM_F32, t.stride(0) if M > 1 else V
+
+
+def token_logprobs(logits: torch.Tensor, ids: Optional[torch.Tensor], ws: Workspace,
+                   logp: Optional[torch.Tensor] = None, entropy: Optional[torch.Tensor] = None,
+                   top_logp: Optional[torch.Tensor] = None, top_ids: Optional[torch.Tensor] = None,
+                   stats: Optional[torch.Tensor] = None, temperature: float = 1.0,
+                   dev_err: Optional[torch.Tensor] = None, stream=None):
+    """Log-probabilities of ids [M] under softmax(logits / temperature) for logits [M, V], entropies, the
+    top_ids.shape[1] most likely ids, and the statistics [M, 2] for token_logprobs_grad (see gm.h)."""
+    pz, dt, ld = _logit_rows(logits, "logits")
+    M, V = logits.shape
+    topk = 0
+    if ids is not None:
+        _need(ids, torch.int32, (M,), "ids")
+    for t, name in ((logp, "logp"), (entropy, "entropy")):
+        if t is not None:
+            _need(t, torch.float32, (M,), name)
+    if stats is not None:
+        _need(stats, torch.float32, (M, 2), "stats")
+    if top_ids is not None and top_logp is not None:
+        topk = top_ids.shape[-1]
+        _need(top_ids, torch.int32, (M, topk), "top_ids")
+        _need(top_logp, torch.float32, (M, topk), "top_logp")
+    cfg = ModelConfig()
+    cfg.vocab = V
+    buf = ws.get(workspace_size(GM_OP_TOKEN_LOGPROBS, cfg, M, topk, 0))
+    _check(lib().gm_token_logprobs(M, V, dt, pz, ld, temperature, _ptr(ids), _ptr(logp), _ptr(entropy), topk,
+                                   _ptr(top_logp), _ptr(top_ids), _ptr(stats), _ptr(buf), buf.numel(), _ptr(dev_err),
+                                   _stream(stream)))
+
+
+def token_logprobs_grad(logits: torch.Tensor, ids: Optional[torch.Tensor], stats: torch.Tensor,
+                        g_logp: Optional[torch.Tensor], grad: torch.Tensor, entropy: Optional[torch.Tensor] = None,
+                        g_entropy: Optional[torch.Tensor] = None, temperature: float = 1.0, stream=None):
+    """The gradient of token_logprobs' logp and entropy in the logits, into grad [M, V] (see gm.h)."""
+    pz, dt, ld = _logit_rows(logits, "logits")
+    pg, dg, ldg = _logit_rows(grad, "grad")
+    M, V = logits.shape
+    if dg != dt or grad.shape != logits.shape:
+        raise ValueError("grad: expected %s %s, got %s %s" % (logits.dtype, (M, V), grad.dtype, tuple(grad.shape)))
+    if ids is not None:
+        _need(ids, torch.int32, (M,), "ids")
+    _need(stats, torch.float32, (M, 2), "stats")
+    for t, name in ((g_logp, "g_logp"), (entropy, "entropy"), (g_entropy, "g_entropy")):
+        if t is not None:
+            _need(t, torch.float32, (M,), name)
+    _check(lib().gm_token_logprobs_grad(M, V, dt, pz, ld, temperature, _ptr(ids), _ptr(stats), _ptr(entropy),
+                                        _ptr(g_logp), _ptr(g_entropy), pg, ldg, _stream(stream)))
 
 
 # ------------------------------------------------------------------------ kernel timing
