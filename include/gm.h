@@ -473,7 +473,7 @@ typedef struct {
  *   top_logp, top_ids [M][topk] (both or neither): the topk largest logits' log p and
  *     ids, in decreasing logit, equal logits in increasing id; 1 <= topk <= min(64, V).
  *   stats [M]: for gm_token_logprobs_grad.
- * Sums are float32 over at most 64 ids and float64 beyond.  Logits of -inf have
+ * Sums are float32 over at most 8192 ids, added pairwise in part, and float64 beyond.  Logits of -inf have
  * probability 0; a log p below float32's range is -inf.  A row without any other logit: log p -inf, entropy 0, stats (-inf, 0),
  * alternatives 0 .. topk-1.  A row that holds NaN or +inf gives NaN log p and entropy,
  * and alternatives -1.

@@ -161,14 +161,10 @@ void launch_residual_draw(const char *chunk_name, const char *scan_name, int B, 
                           double *wsum, double *psum, bool nucleus, hipStream_t s);
 
 // ---------------------------------------------------------------- token log-probabilities (logprob.hip)
-constexpr int kLpChunk = 16384;     // ids per workgroup of the forward pass
+constexpr int kLpMaxParts = 512;    // stretches of a row
 constexpr int kLpMaxTopk = 64;
 constexpr int kLpMaxRows = 1 << 23; // rows per call: a workgroup each of 256 threads, less than 2^32 threads per launch
-inline int lp_chunks(int V) { return (V + kLpChunk - 1) / kLpChunk; }
-// Ids per run maximum of the alternatives' selection: at least 64 runs down to 512 ids, so that the runs'
-// maxima bound the 64th best logit, and at most 2048 of them, 32 per lane of a wave.
-inline int lp_run(int V) { return V > 16384 ? 256 : V > 2048 ? 32 : 8; }
-inline int lp_runs(int V) { return (V + lp_run(V) - 1) / lp_run(V); }
+constexpr int kLpMaxGroups = 2048;  // groups of ids whose maxima the alternatives' selection takes
 struct LpOut {          // outputs of gm_token_logprobs; any may be null
   const int32_t *ids;
   float *logp, *entropy, *top_logp;

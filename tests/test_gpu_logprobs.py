@@ -1,9 +1,9 @@
 """Token log-probabilities and their gradient on the GPU against float64.
 
 Tolerances, u = 2^-24 (half a float32 step).  With y = (z - max) / T in units of log 2: a term exp2(y) is off by
-(3 |y| ln 2 + 2) u (difference, scale and product each by u; the exponential by 2 u), a float32 partial sum of at
-most 64 terms by 64 u, float64 beyond: S and log S by at most (3 E|y| + 68) u with E the mean under p; W / S
-by (3 E y^2 + 136 E|y| + 3 (E|y|)^2) u.  The quotients and the last rounding add 4 u of the value.
+(3 |y| ln 2 + 2) u (difference, scale and product each by u; the exponential by 2 u), a lane's float32 sum of at
+most 64 terms by 64 u, the sum of a lane's two and of 64 lanes by pairs by 7 u more, float64 beyond: S and log S
+by at most (3 E|y| + 73) u with E the mean under p, 78 taken; W / S by (3 E y^2 + 156 E|y| + 3 (E|y|)^2) u.  The quotients and the last rounding add 4 u of the value.
 """
 import math
 
@@ -107,12 +107,12 @@ def test_forward(M, V, dtype, T, topk, kind, ld):
     for a in (w_logp, w_lp):
         a[a <= -(2.0 ** 128) * (1 - 2.0 ** -25)] = -np.inf
     e1, e2, _, _ = _moments(z, T)
-    ds = (3 * e1 + 68) * U
+    ds = (3 * e1 + 78) * U
     got = logp.cpu().numpy()
     live = np.isfinite(w_logp)
     assert np.array_equal(got[~live], w_logp[~live])
     assert (np.abs(got[live] - w_logp[live]) <= (ds + 4 * U * np.abs(w_logp))[live]).all()
-    dh = ds + (3 * e2 + 136 * e1 + 3 * e1 * e1) * U + 4 * U * w_ent
+    dh = ds + (3 * e2 + 156 * e1 + 3 * e1 * e1) * U + 4 * U * w_ent
     assert (np.abs(ent.cpu().numpy() - w_ent) <= dh).all()
     st = stats.cpu().numpy()
     assert np.array_equal(st[:, 0], mx.astype(np.float32))
@@ -179,7 +179,7 @@ GRAD = [
 @pytest.mark.parametrize("M,V,dtype,T,entropy,tokens,kind,ld", GRAD)
 def test_gradient(M, V, dtype, T, entropy, tokens, kind, ld):
     """Against the formula.  A value is e (a + b y) with e as above, a and b off by (S, quotients, entropy)
-    at most (3 E|y| + 80 + dH) u of their terms; then the gradient's own type."""
+    at most (3 E|y| + 90 + dH) u of their terms; then the gradient's own type."""
     need_gpu()
     t, z = _logits(M, V, dtype, V + 1, kind, ld)
     r = np.random.default_rng(V + 1)
@@ -202,7 +202,7 @@ def test_gradient(M, V, dtype, T, entropy, tokens, kind, ld):
     gg = np.abs(g) * (ids >= 0) * tokens
     hh = np.abs(gh) * entropy
     terms = gg[:, None] + hh[:, None] * (a + w_ent[:, None] + np.log(np.maximum(S, 1))[:, None])
-    c = 3 * a + (3 * e1 + 80)[:, None] + (3 * e2 + 136 * e1 + 3 * e1 * e1)[:, None]
+    c = 3 * a + (3 * e1 + 90)[:, None] + (3 * e2 + 156 * e1 + 3 * e1 * e1)[:, None]
     half = 2.0 ** -8 if dtype == torch.bfloat16 else U
     step = half * np.abs(want) + (U * c * p * terms + 4 * U * gg[:, None] * (np.arange(V) == ids[:, None])) / T
     tiny = 2.0 ** -133 if dtype == torch.bfloat16 else 2.0 ** -125      # below the smallest normal values
