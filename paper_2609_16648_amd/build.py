@@ -30,6 +30,7 @@ CFLAGS = ["-O3", "-std=c++17", "-fPIC", "--offload-arch=" + ARCH, "-Wall", "-Wno
 # in gemm.hip the register rings otherwise lose their fixed registers across
 # loop turns (the accumulators get shuffled through copies every iteration).
 EXTRA_FLAGS = {"attention.hip": ["-mllvm", "--amdgpu-mfma-vgpr-form"],
+               "tree_attention.hip": ["-mllvm", "--amdgpu-mfma-vgpr-form"],
                "gemm.hip": ["-mllvm", "--amdgpu-mfma-vgpr-form"]}
 
 

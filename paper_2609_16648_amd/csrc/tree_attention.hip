@@ -1,0 +1,492 @@
+// Attention of a draft tree's nodes over the cache: node i of sequence b attends to the committed positions and
+// to the nodes of its mask (its ancestors and itself).  The rows of a KV head are its query heads times the
+// nodes, (n_heads / n_kv_heads) * N, up to 4096.
+//
+// Up to 32 rows: the kernel of the verify attention (attention.h), whose waves stream K and V straight into
+// operand registers, one wave per KV head; bound by HBM.
+// More rows (tree_attn_kernel): a wave holds 64 rows, so that a KV tile read from LDS serves 64 queries; a
+// workgroup's four waves are four heads of up to 64 rows, two of up to 128 or one of up to 256 (further rows: further
+// workgroups), and the workgroup brings each tile into LDS once for all of them.
+//  * S^T = K Q^T and O^T = V^T P^T on v_mfma_f32_32x32x16_bf16: a lane holds half of the tokens of one query,
+//    so a row's maximum takes one exchange between lanes and P goes into the second product without one.
+//  * K and V go from memory into LDS without passing registers, in stages of 32 tokens (a pair of tiles) of the
+//    workgroup's heads, 128 KiB of them: 2, 4 or 8 stages, all but the one being read in flight.
+//    Four heads: each wave brings its own head's tiles, reads a stage's operands into registers at once
+//    and gives its place to the stage after next; no wave waits for another.  Fewer heads: a barrier per stage
+//    says that the stage has arrived for all waves and that the one before it has been read.
+//  * The operands of a stage are asked for together, before its first product.
+//  * P is split into bf16 hi + lo parts, two products per V operand: the weights keep 16 bits.
+//  * Work partition, partials and their combination are the verify attention's.
+#include "attention.h"
+
+namespace gm {
+
+namespace {
+typedef float f32x16_t __attribute__((ext_vector_type(16)));
+
+constexpr int kTreeLds = 128 * 1024;      // bytes of the stages
+constexpr int kTreeBlock = 256;
+
+// 16 bytes per lane from memory into LDS at lds + 16 * lane (lds uniform), counted in vmcnt.  In asm, so that the
+// compiler does not put a wait for it before every LDS read (it cannot tell the stages apart): the
+// kernel waits itself (wait_loads).  No register is written.
+__device__ __forceinline__ void load_to_lds(uint32_t lds, const uint16_t *src) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off nt" ::"s"(lds), "v"(src) : "memory");
+}
+// until at most n vector memory operations of this wave are under way (older ones complete first)
+template <int n> __device__ __forceinline__ void wait_vm() {
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(n) : "memory");
+}
+
+// HG: heads per workgroup
+template <int HG>
+__global__ __launch_bounds__(kTreeBlock) void tree_attn_kernel(AttnK a) {
+  constexpr int WPH = 4 / HG;                    // waves per head
+  constexpr int kStage = HG * 16384, kRing = kTreeLds / kStage;
+  constexpr int kLoads = 4 * HG;                 // loads per wave and stage
+  constexpr int kLater = HG == 4 ? 1 : kRing - 2;   // stages behind the awaited one that may be under way
+  __shared__ int scan_sh[16];
+  __shared__ int cum_sh[kTreeBlock + 1], m0_sh[kTreeBlock], bl_sh[kTreeBlock];
+  __shared__ int slot_sh[kAttnWinTiles], seq_sh[kAttnWinTiles];
+  // per stage K tiles [HG][2], then V tiles [HG][2], as they lie in the pool
+  extern __shared__ __attribute__((aligned(16))) uint8_t stage_sh[];
+
+  const int tid = threadIdx.x, lane = tid & 63, j = lane & 31, g = lane >> 5;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int part = blockIdx.x, kvh0 = blockIdx.y * HG, hw = w / WPH, kvh = kvh0 + hw;
+  const int rows = a.G * a.R, row0 = ((int)blockIdx.z * WPH + w % WPH) * 64;
+  const bool wave_ok = kvh < a.n_kv && row0 < rows;    // other waves only bring tiles
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void *)stage_sh;
+
+  const bool one_chunk = a.B <= kTreeBlock, writer = part == 0 && blockIdx.y == 0 && blockIdx.z == 0;
+  int TT = 0, T1 = 0, cb1 = 0, m1 = 0, r1 = 0;
+  if (one_chunk) {
+    T1 = tid < a.B ? seq_tiles(a, tid, m1, r1) : 0;
+    cb1 = block_excl_scan(T1, scan_sh, &TT);
+    if (writer && tid < a.B) a.cum[tid] = cb1;
+  } else {
+    for (int c = 0; c < a.B; c += kTreeBlock) {
+      const int T = c + tid < a.B ? seq_tiles(a, c + tid, m1, r1) : 0;
+      int tot;
+      const int cb = TT + block_excl_scan(T, scan_sh, &tot);
+      if (writer && c + tid < a.B) a.cum[c + tid] = cb;
+      TT += tot;
+    }
+  }
+  if (writer && tid == 0) a.cum[a.B] = TT;
+  const int s = part_begin(part, TT, a.parts), e = part_begin(part + 1, TT, a.parts);
+  if (s >= e) return;
+  const int tpp = a.page_size >> 4;
+
+  // this lane's queries: rows row0 + 32 t + j
+  int qi[2], qoff[2];
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    const int r = row0 + 32 * t + j;
+    qi[t] = r < rows && wave_ok ? r % a.R : -1;
+    qoff[t] = qi[t] >= 0 ? (qi[t] * a.n_heads + kvh * a.G + r / a.R) * 128 : 0;
+  }
+  // the segment being computed (see attn_mfma_kernel)
+  int b = -1, m0 = 0, L = 0, cb = 0, seq_end = 0;
+  bool dead = false;
+  uint32_t wild = 0;
+  bf16x8_t qf[2][8];
+  unsigned long long anc[2];
+  bool node[2];
+  float m[2], l[2];
+  f32x16_t O[2][4];
+
+  auto begin = [&](int c, int q) {
+    b = c + q;
+    m0 = __builtin_amdgcn_readfirstlane(m0_sh[q]);
+    const int blen = __builtin_amdgcn_readfirstlane(bl_sh[q]);
+    L = m0 + blen;
+    cb = __builtin_amdgcn_readfirstlane(cum_sh[q]);
+    seq_end = __builtin_amdgcn_readfirstlane(cum_sh[q + 1]);
+    dead = false;
+    wild = 0;
+    const uint16_t *qb = a.q + (long)b * a.R * a.n_heads * 128;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      node[t] = qi[t] >= 0 && qi[t] < blen;
+      anc[t] = node[t] ? a.masks[(long)b * a.R + qi[t]] : 0ull;
+      if (blen < kMaxNodes) anc[t] &= (1ull << blen) - 1;
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        qf[t][k] = as_bf16x8(qi[t] >= 0 ? *reinterpret_cast<const uint4 *>(qb + qoff[t] + 16 * k + 8 * g)
+                                        : make_uint4(0, 0, 0, 0));
+      m[t] = -INFINITY;
+      l[t] = 0.f;
+#pragma unroll
+      for (int q4 = 0; q4 < 4; ++q4)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) O[t][q4][i] = 0.f;
+    }
+  };
+  auto finish = [&]() {
+    const bool whole = cb >= s && seq_end <= e;
+    if (wild) {
+      // V that is inf or NaN stayed out of the products (0 * inf is NaN): added here, weight aside, for the rows
+      // that see its token
+#pragma unroll 1
+      for (int tok = m0 & ~15; tok < L; ++tok) {
+        const int tile = tok >> 4, d = tok - m0;
+        if (!(wild >> (tile - m0 / 16) & 1)) continue;
+        const int page = a.bt[(long)b * a.max_pages + tile / tpp];
+        const uint16_t *v = a.vp + ((long)page * a.n_kv + kvh) * a.page_size * 128 + (long)(tile % tpp) * 2048;
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const float f = bf16_to_f32(v[v_tile_off(tok & 15, 32 * c + 8 * (i >> 2) + 4 * g + (i & 3))]);
+            if (!(fabsf(f) < INFINITY)) {
+#pragma unroll
+              for (int t = 0; t < 2; ++t)
+                if ((d < 0) | bool(anc[t] >> (d & 63) & 1)) O[t][c][i] += f;
+            }
+          }
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const float lu = l[t] + __shfl_xor(l[t], 32, kWave);
+      const int r = row0 + 32 * t + j;
+      if (qi[t] < 0) continue;
+      if (!whole) {
+        const long prow = ((long)(part + b) * a.n_kv + kvh) * a.rows_pad + r;
+        if (g == 0) a.part_ml[prow] = make_float2(m[t], lu);
+        float *dst = a.part_o + prow * 128 + 4 * g;
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            *reinterpret_cast<floatx4_t *>(dst + 32 * c + 8 * i) =
+                floatx4_t{O[t][c][4 * i], O[t][c][4 * i + 1], O[t][c][4 * i + 2], O[t][c][4 * i + 3]};
+      } else {
+        const bool live = node[t] && m[t] != -INFINITY;
+        const float inv = 1.f / lu;
+        uint16_t *dst = a.out + (long)b * a.R * a.n_heads * 128 + qoff[t] + 4 * g;
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            float f[4];
+#pragma unroll
+            for (int x = 0; x < 4; ++x) f[x] = live ? O[t][c][4 * i + x] * inv : 0.f;
+            *reinterpret_cast<uint2 *>(dst + 32 * c + 8 * i) = make_uint2(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]));
+          }
+      }
+    }
+  };
+
+  // The tokens tb .. tb + 31, of which those below lim are there, for this wave's rows.  `release` is called as soon
+  // as the stage's operands are in registers.
+  auto block = [&](const uint8_t *st, int tb, int lim, bool mask, auto release) {
+    const uint8_t *kt = st + hw * 8192, *vt = st + HG * 8192 + hw * 8192;
+    bf16x8_t kf[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      kf[k] = as_bf16x8(*reinterpret_cast<const uint4 *>(kt + (j >> 4) * 4096 + (2 * k + g) * 256 + (j & 15) * 16));
+    __builtin_amdgcn_sched_barrier(0);
+    f32x16_t S[2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) S[t][i] = 0.f;
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+#pragma unroll
+      for (int t = 0; t < 2; ++t) S[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[k], qf[t][k], S[t], 0, 0, 0);
+    uint4 vf[2][4];       // tokens 4 g .. + 3 and 8 + 4 g .. + 3 of tile k, channel 32 c + j
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const uint8_t *p = vt + k * 4096 + c * 1024 + g * 256 + (j & 15) * 16 + (j >> 4) * 8;
+        const uint2 x = *reinterpret_cast<const uint2 *>(p), y = *reinterpret_cast<const uint2 *>(p + 512);
+        vf[k][c] = make_uint4(x.x, x.y, y.x, y.y);
+      }
+    __builtin_amdgcn_sched_barrier(0);
+    release();
+    if (mask) {
+      // entries past the last node are nothing; nodes' values that are inf or NaN are kept for the end (finish)
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const bool nodes = tb + 16 * k + 16 > m0;
+        bool mine = false;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          uint32_t v[4] = {vf[k][c].x, vf[k][c].y, vf[k][c].z, vf[k][c].w};
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int left = lim - (tb + 16 * k + 8 * (i >> 1) + 4 * g + 2 * (i & 1));
+            v[i] = left <= 0 ? 0u : left == 1 ? v[i] & 0x0000ffffu : v[i];
+            const uint32_t f = finite_or_0(v[i]);
+            mine = mine | (f != v[i]);
+            v[i] = nodes ? f : v[i];
+          }
+          vf[k][c] = make_uint4(v[0], v[1], v[2], v[3]);
+        }
+        if (nodes && __any(mine)) wild |= 1u << (tb / 16 + k - m0 / 16);
+      }
+    }
+    // S[t][4 i + r]: token tb + 8 i + 4 g + r, query 32 t + j
+    float tmax[2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      if (mask) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          // without branches: the tile's 32 tests are a few instructions each
+          const int tok = tb + 8 * (i >> 2) + 4 * g + (i & 3), d = tok - m0;
+          const bool seen = (tok < lim) & ((d < 0) | ((d < kMaxNodes) & bool(anc[t] >> (d & 63) & 1)));
+          S[t][i] = seen ? S[t][i] : -INFINITY;
+        }
+      }
+      float x0 = fmaxf(S[t][0], S[t][1]);
+#pragma unroll
+      for (int i = 2; i < 16; i += 2) x0 = fmaxf(x0, fmaxf(S[t][i], S[t][i + 1]));
+      tmax[t] = fmaxf(x0, __shfl_xor(x0, 32, kWave)) * a.scale_log2;
+    }
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const bool up = tmax[t] > m[t] + kLazyLog2;
+      if (__any(up)) {
+        const float mn = up ? fmaxf(m[t], tmax[t]) : m[t];
+        const float alpha = (!up || mn == -INFINITY) ? 1.f : __builtin_amdgcn_exp2f(m[t] - mn);
+        l[t] *= alpha;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) O[t][c] *= alpha;
+        m[t] = mn;
+      }
+    }
+    bf16x8_t hi[2][2], lo[2][2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const float ref = m[t] == -INFINITY ? 0.f : m[t];     // (a row that has seen nothing: every score is -inf)
+      float p[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(S[t][i], a.scale_log2, -ref));
+        l[t] += p[i];
+      }
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        uint32_t h[4], q[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float p0 = p[8 * k + 2 * i], p1 = p[8 * k + 2 * i + 1];
+          h[i] = pack_bf16(p0, p1);
+          q[i] = pack_bf16(p0 - __uint_as_float(h[i] << 16), p1 - __uint_as_float(h[i] & 0xffff0000u));
+        }
+        hi[t][k] = as_bf16x8(make_uint4(h[0], h[1], h[2], h[3]));
+        lo[t][k] = as_bf16x8(make_uint4(q[0], q[1], q[2], q[3]));
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) O[t][c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(vf[k][c]), hi[t][k], O[t][c], 0, 0, 0);
+#pragma unroll
+        for (int t = 0; t < 2; ++t) O[t][c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(vf[k][c]), lo[t][k], O[t][c], 0, 0, 0);
+      }
+  };
+
+  // Stage the pair of tiles at i of the window (n of them, 1 or 2; the second's place is filled with the first again)
+  // into place p.
+  auto fetch = [&](int i, int n, int p) {
+#pragma unroll
+    for (int q = 0; q < HG; ++q) {
+      // this wave's unit of 4 KiB: of its own head (HG = 4), else of units w HG + q: K or V, head, tile
+      const int u = HG == 4 ? (q >> 1) * 8 + hw * 2 + (q & 1) : w * HG + q;
+      const int t = u & 1, h = (u >> 1) % HG, kv = u / (2 * HG);
+      const int head = min(kvh0 + h, a.n_kv - 1);
+      const int slot = max(0, __builtin_amdgcn_readfirstlane(slot_sh[i + min(t, n - 1)]));
+      const uint16_t *src = (kv ? a.vp : a.kp) + (long)head * a.page_size * 128 + (long)slot * 2048 + lane * 8;
+      const uint32_t dst = lds0 + p * kStage + u * 4096;
+#pragma unroll
+      for (int x = 0; x < 4; ++x) load_to_lds(dst + x * 1024, src + x * 512);
+    }
+  };
+  // until the oldest stage under way has arrived, with `later` stages fetched behind it
+  auto arrived = [&](int later) {
+    if (later >= kLater) wait_vm<kLater * kLoads>();
+    else if (HG == 1 && later == 5) wait_vm<5 * kLoads>();
+    else if (HG == 1 && later == 4) wait_vm<4 * kLoads>();
+    else if (HG == 1 && later == 3) wait_vm<3 * kLoads>();
+    else if (HG == 1 && later == 2) wait_vm<2 * kLoads>();
+    else if (HG <= 2 && later == 1) wait_vm<kLoads>();
+    else wait_vm<0>();
+  };
+
+  int run = 0;
+  for (int c = 0; c < a.B; c += kTreeBlock) {
+    int T, cbt, tot;
+    if (one_chunk) {
+      T = T1;
+      cbt = cb1;
+      tot = TT;
+    } else {
+      T = c + tid < a.B ? seq_tiles(a, c + tid, m1, r1) : 0;
+      cbt = run + block_excl_scan(T, scan_sh, &tot);
+    }
+    const int cbeg = run, cend = run + tot;
+    run = cend;
+    if (cend <= s) continue;
+    if (cbeg >= e) break;
+    __syncthreads();
+    cum_sh[tid] = cbt;
+    if (tid == 0) cum_sh[kTreeBlock] = cend;
+    m0_sh[tid] = m1;
+    bl_sh[tid] = r1;
+    const int xe = min(e, cend);
+    for (int x0 = max(s, cbeg); x0 < xe; x0 += kAttnWinTiles) {
+      const int nt = min(kAttnWinTiles, xe - x0);
+      __syncthreads();
+      for (int i = tid; i < nt; i += kTreeBlock) {
+        int lo = 0, hi = min(kTreeBlock, a.B - c);
+        while (hi - lo > 1) {
+          const int mid = (lo + hi) >> 1;
+          if (cum_sh[mid] <= x0 + i) lo = mid;
+          else hi = mid;
+        }
+        const int t = x0 + i - cum_sh[lo], pi = t / tpp;
+        const int page = pi < a.max_pages ? a.bt[(long)(c + lo) * a.max_pages + pi] : -1;
+        const bool ok = page >= 0 && page < a.num_pages;
+        if (!ok) raise_dev_err(a.dev_err, GM_DEVERR_PAGE);
+        seq_sh[i] = lo;
+        slot_sh[i] = ok ? page * a.n_kv * tpp + t % tpp : -1;
+      }
+      __syncthreads();
+      // a stage: the tiles i .. i + n - 1 of the window, all of one sequence
+      auto pair_of = [&](int i) {
+        const int q = __builtin_amdgcn_readfirstlane(seq_sh[i]);
+        return min(2, min(nt, __builtin_amdgcn_readfirstlane(cum_sh[q + 1]) - x0) - i);
+      };
+      int i = 0, next = 0, ahead = 0, place = 0;    // the stage computed; the next to fetch; fetched ones from i on
+      auto fetch_next = [&]() {
+        if (next >= nt) return;
+        const int n = pair_of(next);
+        fetch(next, n, (place + ahead) % kRing);
+        next += n;
+        ++ahead;
+      };
+      for (int f = 0; f < (HG == 4 ? 2 : kRing - 1); ++f) fetch_next();
+      while (i < nt) {
+        const int n = pair_of(i);
+        arrived(ahead - 1);
+        if (HG < 4) {
+          __builtin_amdgcn_s_barrier();
+          asm volatile("" ::: "memory");
+          fetch_next();
+        }
+        const uint8_t *st = stage_sh + place * kStage;
+        auto release = [&]() {
+          if (HG < 4) return;
+          asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+          fetch_next();
+        };
+        // (waves without rows compute along: what they hold is written nowhere)
+        const int q = __builtin_amdgcn_readfirstlane(seq_sh[i]);
+        if (b != c + q) begin(c, q);
+        int there = n;
+        if (there > 1 && __builtin_amdgcn_readfirstlane(slot_sh[i + 1]) < 0) there = 1;
+        if (__builtin_amdgcn_readfirstlane(slot_sh[i]) < 0) there = 0;
+        if (dead) there = 0;
+        dead = there < n;
+        const int tb = 16 * (x0 + i - cb);
+        block(st, tb, min(L, tb + 16 * there), there < 2 || tb + 32 > m0, release);
+        i += n;
+        --ahead;
+        place = (place + 1) % kRing;
+        if (wave_ok && x0 + i == min(e, seq_end)) finish();
+      }
+      wait_vm<0>();
+    }
+  }
+}
+
+// Row tiles of a KV head: up to two go to attn_mfma_kernel; more, in 64s, to waves of tree_attn_kernel.
+struct TreeGeom {
+  bool wide;
+  int heads_per_group, groups, row_groups, rows_pad, block, rt;
+};
+TreeGeom tree_geom(int rows, int n_kv) {
+  TreeGeom g;
+  g.wide = rows > 32;
+  g.rt = rows <= 16 ? 1 : 2;
+  g.heads_per_group = !g.wide || rows <= 64 ? 4 : rows <= 128 ? 2 : 1;
+  g.row_groups = g.wide ? (rows + 255) / 256 : 1;
+  g.rows_pad = g.wide ? (rows + 63) / 64 * 64 : g.rt * 16;
+  if (!g.wide && g.heads_per_group > n_kv) g.heads_per_group = n_kv;
+  g.groups = (n_kv + g.heads_per_group - 1) / g.heads_per_group;
+  g.block = g.wide ? kTreeBlock : 64 * g.heads_per_group;
+  return g;
+}
+
+// kernels that reserve more LDS than a launch may by itself say so once per device
+template <typename F>
+void reserve(F *kernel, int bytes, std::atomic<uint32_t> &ready) {
+  int dev = 0;
+  if (hipGetDevice(&dev) != hipSuccess) dev = 31;
+  if (dev < 31 && (ready.load() >> dev & 1)) return;
+  (void)hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (dev < 31) ready.fetch_or(1u << dev);
+}
+template <int RT>
+void launch_narrow(const AttnK &k, const TreeGeom &g, hipStream_t s) {
+  static std::atomic<uint32_t> ready{0};
+  reserve(attn_mfma_kernel<true, RT, true>, kAttnLdsReserve, ready);
+  hipLaunchKernelGGL((attn_mfma_kernel<true, RT, true>), dim3(k.parts, g.groups), dim3(g.block), kAttnLdsReserve, s, k);
+}
+template <int HG>
+void launch_wide(const AttnK &k, const TreeGeom &g, hipStream_t s) {
+  static std::atomic<uint32_t> ready{0};
+  reserve(tree_attn_kernel<HG>, kTreeLds, ready);
+  hipLaunchKernelGGL(tree_attn_kernel<HG>, dim3(k.parts, g.groups, g.row_groups), dim3(kTreeBlock), kTreeLds, s,
+                     k);
+}
+}  // namespace
+
+AttnPlan plan_tree_attention(const gm_model_config &cfg, int B, int N) {
+  AttnPlan p{};
+  if (cfg.dtype != GM_BF16) return p;
+  const TreeGeom g = tree_geom(cfg.n_heads / cfg.n_kv_heads * N, cfg.n_kv_heads);
+  p.rows_pad = g.rows_pad;
+  const int parts = attn_resident_groups(g.block) / (g.groups * g.row_groups);
+  p.parts = parts < 1 ? 1 : parts;
+  Carve c;     // the partial of (range p, sequence b) is in slot p + b
+  const size_t n = (size_t)(p.parts + B) * cfg.n_kv_heads * p.rows_pad;
+  p.part_o = c.take(n * 128 * sizeof(float));
+  p.part_ml = c.take(n * sizeof(float2));
+  p.cum = c.take((size_t)(B + 1) * sizeof(int32_t));
+  p.total = c.off;
+  return p;
+}
+
+void run_tree_attention(const AttnArgs &a, const uint64_t *masks, const AttnPlan &p, char *ws, hipStream_t s) {
+  if (a.B == 0) return;
+  if (a.dtype != GM_BF16) {
+    launch_attn_f32<true>(a, masks, s);
+    return;
+  }
+  const TreeGeom g = tree_geom(a.n_heads / a.n_kv * a.R, a.n_kv);
+  AttnGeom geo{};
+  geo.heads_per_group = g.heads_per_group;
+  geo.waves_per_head = 1;
+  AttnK k = attn_k(a, p, geo, ws);
+  k.masks = (const unsigned long long *)masks;
+  {
+    TraceScope ts(a.trace, s);
+    if (g.wide && g.heads_per_group == 4) launch_wide<4>(k, g, s);
+    else if (g.wide && g.heads_per_group == 2) launch_wide<2>(k, g, s);
+    else if (g.wide) launch_wide<1>(k, g, s);
+    else if (g.rt == 1) launch_narrow<1>(k, g, s);
+    else launch_narrow<2>(k, g, s);
+  }
+  launch_attn_combine(k, a.trace_combine, s);
+}
+
+}  // namespace gm
