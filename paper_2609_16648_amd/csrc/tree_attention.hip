@@ -27,11 +27,17 @@ typedef float f32x16_t __attribute__((ext_vector_type(16)));
 constexpr int kTreeLds = 128 * 1024;      // bytes of the stages
 constexpr int kTreeBlock = 256;
 
-// 16 bytes per lane from memory into LDS at lds + 16 * lane (lds uniform), counted in vmcnt.  In asm, so that the
-// compiler does not put a wait for it before every LDS read (it cannot tell the stages apart): the
-// kernel waits itself (wait_loads).  No register is written.
-__device__ __forceinline__ void load_to_lds(uint32_t lds, const uint16_t *src) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off nt" ::"s"(lds), "v"(src) : "memory");
+// 4 KiB from memory (uniform) into LDS (uniform), 4 x 16 bytes per lane, counted in vmcnt; off = 16 * lane.  In asm, so
+// that the compiler does not put a wait for it before every LDS read (it cannot tell the stages apart): the
+// kernel waits itself (wait_vm).  No register is written.  The instructions' offsets count on both sides.
+__device__ __forceinline__ void load_to_lds(uint32_t lds, const uint16_t *src, uint32_t off) {
+  asm volatile(
+      "s_mov_b32 m0, %0\n\ts_nop 0\n\t"
+      "global_load_lds_dwordx4 %2, %1 nt\n\t"
+      "global_load_lds_dwordx4 %2, %1 offset:1024 nt\n\t"
+      "global_load_lds_dwordx4 %2, %1 offset:2048 nt\n\t"
+      "global_load_lds_dwordx4 %2, %1 offset:3072 nt" ::"s"(lds), "s"(src), "v"(off)
+      : "memory");
 }
 // until at most n vector memory operations of this wave are under way (older ones complete first)
 template <int n> __device__ __forceinline__ void wait_vm() {
@@ -44,10 +50,12 @@ __global__ __launch_bounds__(kTreeBlock) void tree_attn_kernel(AttnK a) {
   constexpr int WPH = 4 / HG;                    // waves per head
   constexpr int kStage = HG * 16384, kRing = kTreeLds / kStage;
   constexpr int kLoads = 4 * HG;                 // loads per wave and stage
-  constexpr int kLater = HG == 4 ? 1 : kRing - 2;   // stages behind the awaited one that may be under way
+  constexpr bool kEarly = HG < 4;                // K's operands are read a stage ahead
+  constexpr int kLater = kEarly ? kRing - 3 : 1;   // stages behind the awaited one that may be under way
   __shared__ int scan_sh[16];
   __shared__ int cum_sh[kTreeBlock + 1], m0_sh[kTreeBlock], bl_sh[kTreeBlock];
-  __shared__ int slot_sh[kAttnWinTiles], seq_sh[kAttnWinTiles];
+  __shared__ int slot_sh[kAttnWinTiles];
+  __shared__ int4 list_sh[kAttnWinTiles];        // the window's stages (struct Stage)
   // per stage K tiles [HG][2], then V tiles [HG][2], as they lie in the pool
   extern __shared__ __attribute__((aligned(16))) uint8_t stage_sh[];
 
@@ -96,6 +104,7 @@ __global__ __launch_bounds__(kTreeBlock) void tree_attn_kernel(AttnK a) {
   float m[2], l[2];
   f32x16_t O[2][4];
 
+  static_assert(kAttnWinTiles <= kTreeBlock, "a thread per tile of a window");
   auto begin = [&](int c, int q) {
     b = c + q;
     m0 = __builtin_amdgcn_readfirstlane(m0_sh[q]);
@@ -179,16 +188,14 @@ __global__ __launch_bounds__(kTreeBlock) void tree_attn_kernel(AttnK a) {
     }
   };
 
-  // The tokens tb .. tb + 31, of which those below lim are there, for this wave's rows.  `release` is called as soon
-  // as the stage's operands are in registers.
-  auto block = [&](const uint8_t *st, int tb, int lim, bool mask, auto release) {
-    const uint8_t *kt = st + hw * 8192, *vt = st + HG * 8192 + hw * 8192;
-    bf16x8_t kf[8];
+  bf16x8_t kf[8];         // K's operands of the stage to be computed
+  auto read_k = [&](const uint8_t *st) {
+    const uint8_t *kt = st + hw * 8192 + (j >> 4) * 4096 + g * 256 + (j & 15) * 16;
 #pragma unroll
-    for (int k = 0; k < 8; ++k)
-      kf[k] = as_bf16x8(*reinterpret_cast<const uint4 *>(kt + (j >> 4) * 4096 + (2 * k + g) * 256 + (j & 15) * 16));
-    __builtin_amdgcn_sched_barrier(0);
-    f32x16_t S[2];
+    for (int k = 0; k < 8; ++k) kf[k] = as_bf16x8(*reinterpret_cast<const uint4 *>(kt + k * 512));
+  };
+  // S[t][4 i + r]: the score of token 8 i + 4 g + r of the stage and query 32 t + j, unscaled
+  auto scores = [&](f32x16_t (&S)[2]) {
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -197,17 +204,21 @@ __global__ __launch_bounds__(kTreeBlock) void tree_attn_kernel(AttnK a) {
     for (int k = 0; k < 8; ++k)
 #pragma unroll
       for (int t = 0; t < 2; ++t) S[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[k], qf[t][k], S[t], 0, 0, 0);
-    uint4 vf[2][4];       // tokens 4 g .. + 3 and 8 + 4 g .. + 3 of tile k, channel 32 c + j
+  };
+  uint4 vf[2][4];         // V's: tokens 4 g .. + 3 and 8 + 4 g .. + 3 of tile k, channel 32 c + j
+  auto read_v = [&](const uint8_t *st) {
+    const uint8_t *vt = st + (HG + hw) * 8192 + g * 256 + (j & 15) * 16 + (j >> 4) * 8;
 #pragma unroll
     for (int k = 0; k < 2; ++k)
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
-        const uint8_t *p = vt + k * 4096 + c * 1024 + g * 256 + (j & 15) * 16 + (j >> 4) * 8;
+        const uint8_t *p = vt + k * 4096 + c * 1024;
         const uint2 x = *reinterpret_cast<const uint2 *>(p), y = *reinterpret_cast<const uint2 *>(p + 512);
         vf[k][c] = make_uint4(x.x, x.y, y.x, y.y);
       }
-    __builtin_amdgcn_sched_barrier(0);
-    release();
+  };
+  // The masks of the tokens tb .. tb + 31, of which those below lim are there, and the rows' maxima brought up to date.
+  auto settle = [&](f32x16_t (&S)[2], int tb, int lim, bool mask) {
     if (mask) {
       // entries past the last node are nothing; nodes' values that are inf or NaN are kept for the end (finish)
 #pragma unroll
@@ -230,7 +241,6 @@ __global__ __launch_bounds__(kTreeBlock) void tree_attn_kernel(AttnK a) {
         if (nodes && __any(mine)) wild |= 1u << (tb / 16 + k - m0 / 16);
       }
     }
-    // S[t][4 i + r]: token tb + 8 i + 4 g + r, query 32 t + j
     float tmax[2];
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
@@ -243,9 +253,10 @@ __global__ __launch_bounds__(kTreeBlock) void tree_attn_kernel(AttnK a) {
           S[t][i] = seen ? S[t][i] : -INFINITY;
         }
       }
-      float x0 = fmaxf(S[t][0], S[t][1]);
+      // the larger of a pair as the median with infinity: fmaxf would first canonicalise every product's result
+      float x0 = __builtin_amdgcn_fmed3f(S[t][0], S[t][1], INFINITY);
 #pragma unroll
-      for (int i = 2; i < 16; i += 2) x0 = fmaxf(x0, fmaxf(S[t][i], S[t][i + 1]));
+      for (int i = 2; i < 16; i += 2) x0 = fmaxf(x0, __builtin_amdgcn_fmed3f(S[t][i], S[t][i + 1], INFINITY));
       tmax[t] = fmaxf(x0, __shfl_xor(x0, 32, kWave)) * a.scale_log2;
     }
 #pragma unroll
@@ -260,64 +271,72 @@ __global__ __launch_bounds__(kTreeBlock) void tree_attn_kernel(AttnK a) {
         m[t] = mn;
       }
     }
-    bf16x8_t hi[2][2], lo[2][2];
+  };
+  // O += P V; the weights of query tile 1 are computed while the products of tile 0 run, six vector instructions
+  // behind each
+  auto weigh = [&](f32x16_t (&S)[2]) {
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
       const float ref = m[t] == -INFINITY ? 0.f : m[t];     // (a row that has seen nothing: every score is -inf)
-      float p[16];
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(S[t][i], a.scale_log2, -ref));
-        l[t] += p[i];
-      }
+      bf16x8_t hi[2], lo[2];
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
         uint32_t h[4], q[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const float p0 = p[8 * k + 2 * i], p1 = p[8 * k + 2 * i + 1];
+          const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(S[t][8 * k + 2 * i], a.scale_log2, -ref));
+          const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(S[t][8 * k + 2 * i + 1], a.scale_log2, -ref));
+          l[t] += p0;
+          l[t] += p1;
           h[i] = pack_bf16(p0, p1);
           q[i] = pack_bf16(p0 - __uint_as_float(h[i] << 16), p1 - __uint_as_float(h[i] & 0xffff0000u));
         }
-        hi[t][k] = as_bf16x8(make_uint4(h[0], h[1], h[2], h[3]));
-        lo[t][k] = as_bf16x8(make_uint4(q[0], q[1], q[2], q[3]));
+        hi[k] = as_bf16x8(make_uint4(h[0], h[1], h[2], h[3]));
+        lo[k] = as_bf16x8(make_uint4(q[0], q[1], q[2], q[3]));
+      }
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) O[t][c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(vf[k][c]), hi[k], O[t][c], 0, 0, 0);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) O[t][c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(vf[k][c]), lo[k], O[t][c], 0, 0, 0);
       }
     }
+    __builtin_amdgcn_sched_group_barrier(0x402, 100, 0);
 #pragma unroll
-    for (int k = 0; k < 2; ++k)
-#pragma unroll
-      for (int c = 0; c < 4; ++c) {
-#pragma unroll
-        for (int t = 0; t < 2; ++t) O[t][c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(vf[k][c]), hi[t][k], O[t][c], 0, 0, 0);
-#pragma unroll
-        for (int t = 0; t < 2; ++t) O[t][c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(vf[k][c]), lo[t][k], O[t][c], 0, 0, 0);
-      }
+    for (int i = 0; i < 16; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x402, 6, 0);
+    }
   };
 
-  // Stage the pair of tiles at i of the window (n of them, 1 or 2; the second's place is filled with the first again)
-  // into place p.
-  auto fetch = [&](int i, int n, int p) {
+  // A stage: up to two neighbouring tiles of a sequence, in scalar registers.
+  struct Stage {
+    int slot0, slot1;       // places in the pool (a tile that is absent, or on a bad page: some other one's)
+    int x;                  // first tile
+    int seq, there;         // sequence in the chunk; tiles that are there, up to a bad page
+    bool bad, last;         // a bad page; the segment's last stage
+  };
+  auto stage = [&](const int4 &v) {
+    const int meta = __builtin_amdgcn_readfirstlane(v.z);
+    return Stage{__builtin_amdgcn_readfirstlane(v.x), __builtin_amdgcn_readfirstlane(v.y),
+                 __builtin_amdgcn_readfirstlane(v.w), meta & 255, meta >> 8 & 3, (meta >> 10 & 1) != 0,
+                 (meta >> 11 & 1) != 0};
+  };
+  const uint32_t off = lane * 16;
+  auto fetch = [&](const Stage &f, int p) {
 #pragma unroll
     for (int q = 0; q < HG; ++q) {
       // this wave's unit of 4 KiB: of its own head (HG = 4), else of units w HG + q: K or V, head, tile
       const int u = HG == 4 ? (q >> 1) * 8 + hw * 2 + (q & 1) : w * HG + q;
-      const int t = u & 1, h = (u >> 1) % HG, kv = u / (2 * HG);
-      const int head = min(kvh0 + h, a.n_kv - 1);
-      const int slot = max(0, __builtin_amdgcn_readfirstlane(slot_sh[i + min(t, n - 1)]));
-      const uint16_t *src = (kv ? a.vp : a.kp) + (long)head * a.page_size * 128 + (long)slot * 2048 + lane * 8;
-      const uint32_t dst = lds0 + p * kStage + u * 4096;
-#pragma unroll
-      for (int x = 0; x < 4; ++x) load_to_lds(dst + x * 1024, src + x * 512);
+      const int h = (u >> 1) % HG, kv = u / (2 * HG), head = min(kvh0 + h, a.n_kv - 1);
+      const uint16_t *src = (kv ? a.vp : a.kp) + (long)head * a.page_size * 128 + (long)(f.slot0 + (u & 1) * (f.slot1 - f.slot0)) * 2048;
+      load_to_lds(lds0 + p * kStage + u * 4096, src, off);
     }
   };
-  // until the oldest stage under way has arrived, with `later` stages fetched behind it
+  // until a stage has arrived, with `later` stages fetched behind it (the window's last ones arrive together)
   auto arrived = [&](int later) {
     if (later >= kLater) wait_vm<kLater * kLoads>();
-    else if (HG == 1 && later == 5) wait_vm<5 * kLoads>();
-    else if (HG == 1 && later == 4) wait_vm<4 * kLoads>();
-    else if (HG == 1 && later == 3) wait_vm<3 * kLoads>();
-    else if (HG == 1 && later == 2) wait_vm<2 * kLoads>();
-    else if (HG <= 2 && later == 1) wait_vm<kLoads>();
     else wait_vm<0>();
   };
 
@@ -345,7 +364,8 @@ __global__ __launch_bounds__(kTreeBlock) void tree_attn_kernel(AttnK a) {
     for (int x0 = max(s, cbeg); x0 < xe; x0 += kAttnWinTiles) {
       const int nt = min(kAttnWinTiles, xe - x0);
       __syncthreads();
-      for (int i = tid; i < nt; i += kTreeBlock) {
+      int seq = 0;
+      for (int i = tid; i < nt; i += kTreeBlock) {      // (at most one turn)
         int lo = 0, hi = min(kTreeBlock, a.B - c);
         while (hi - lo > 1) {
           const int mid = (lo + hi) >> 1;
@@ -356,52 +376,68 @@ __global__ __launch_bounds__(kTreeBlock) void tree_attn_kernel(AttnK a) {
         const int page = pi < a.max_pages ? a.bt[(long)(c + lo) * a.max_pages + pi] : -1;
         const bool ok = page >= 0 && page < a.num_pages;
         if (!ok) raise_dev_err(a.dev_err, GM_DEVERR_PAGE);
-        seq_sh[i] = lo;
+        seq = lo;
         slot_sh[i] = ok ? page * a.n_kv * tpp + t % tpp : -1;
       }
+      // the stages: pairs of tiles counted from where the sequence begins in this window
+      const int x = x0 + tid;
+      const bool first = tid < nt && ((x - max(cum_sh[seq], x0)) & 1) == 0;
+      int stages;
+      const int at = block_excl_scan(first, scan_sh, &stages);      // (its barriers also order slot_sh)
+      if (first) {
+        const int end = min(cum_sh[seq + 1], x0 + nt), n = min(2, end - x);
+        const int s0 = slot_sh[tid], s1 = n > 1 ? slot_sh[tid + 1] : s0;
+        const int there = s0 < 0 ? 0 : s1 < 0 ? 1 : n;
+        const bool last = x + n == min(e, cum_sh[seq + 1]);
+        list_sh[at] = make_int4(max(s0, 0), max(s1, 0), seq | there << 8 | (there < n) << 10 | last << 11, x);
+      }
       __syncthreads();
-      // a stage: the tiles i .. i + n - 1 of the window, all of one sequence
-      auto pair_of = [&](int i) {
-        const int q = __builtin_amdgcn_readfirstlane(seq_sh[i]);
-        return min(2, min(nt, __builtin_amdgcn_readfirstlane(cum_sh[q + 1]) - x0) - i);
-      };
-      int i = 0, next = 0, ahead = 0, place = 0;    // the stage computed; the next to fetch; fetched ones from i on
+      // Stage f lies in place f % kRing.  `next` is the next one to fetch: kFetch of them before the first is computed,
+      // then one per stage.
+      constexpr int kFetch = kEarly ? kRing - 1 : 2;
+      int next = min(kFetch, stages);
+      for (int f = 0; f < next; ++f) fetch(stage(list_sh[f]), f);
+      Stage cur = stage(list_sh[0]), ahead = stage(list_sh[min(next, stages - 1)]);
       auto fetch_next = [&]() {
-        if (next >= nt) return;
-        const int n = pair_of(next);
-        fetch(next, n, (place + ahead) % kRing);
-        next += n;
-        ++ahead;
+        if (next < stages) fetch(ahead, next++ % kRing);
       };
-      for (int f = 0; f < (HG == 4 ? 2 : kRing - 1); ++f) fetch_next();
-      while (i < nt) {
-        const int n = pair_of(i);
-        arrived(ahead - 1);
-        if (HG < 4) {
+      if (kEarly) {
+        arrived(next - 1);
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        read_k(stage_sh);
+      }
+      // (waves without rows compute along: what they hold is written nowhere)
+      for (int k = 0; k < stages; ++k) {
+        arrived(next - 1 - (kEarly ? min(k + 1, stages - 1) : k));
+        const int4 cur_v = list_sh[min(k + 1, stages - 1)], ahead_v = list_sh[min(k + kFetch + 1, stages - 1)];
+        const uint8_t *const st = stage_sh + k % kRing * kStage;
+        if (kEarly) {
           __builtin_amdgcn_s_barrier();
           asm volatile("" ::: "memory");
           fetch_next();
         }
-        const uint8_t *st = stage_sh + place * kStage;
-        auto release = [&]() {
-          if (HG < 4) return;
+        if (b != c + cur.seq) begin(c, cur.seq);
+        if (!kEarly) read_k(st);
+        __builtin_amdgcn_sched_barrier(0);
+        f32x16_t S[2];
+        scores(S);
+        read_v(st);
+        if (kEarly) read_k(stage_sh + (k + 1) % kRing * kStage);     // (behind the last stage: nothing that is used)
+        __builtin_amdgcn_sched_barrier(0);
+        if (!kEarly) {
           asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
           fetch_next();
-        };
-        // (waves without rows compute along: what they hold is written nowhere)
-        const int q = __builtin_amdgcn_readfirstlane(seq_sh[i]);
-        if (b != c + q) begin(c, q);
-        int there = n;
-        if (there > 1 && __builtin_amdgcn_readfirstlane(slot_sh[i + 1]) < 0) there = 1;
-        if (__builtin_amdgcn_readfirstlane(slot_sh[i]) < 0) there = 0;
-        if (dead) there = 0;
-        dead = there < n;
-        const int tb = 16 * (x0 + i - cb);
-        block(st, tb, min(L, tb + 16 * there), there < 2 || tb + 32 > m0, release);
-        i += n;
-        --ahead;
-        place = (place + 1) % kRing;
-        if (wave_ok && x0 + i == min(e, seq_end)) finish();
+        }
+        const int there = dead ? 0 : cur.there;
+        dead = dead || cur.bad;
+        const int tb = 16 * (cur.x - cb);
+        const bool last = cur.last;
+        settle(S, tb, min(L, tb + 16 * there), there < 2 || tb + 32 > m0);
+        cur = stage(cur_v);
+        ahead = stage(ahead_v);
+        weigh(S);
+        if (last && wave_ok) finish();
       }
       wait_vm<0>();
     }
