@@ -25,35 +25,45 @@ namespace {
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 
 constexpr int kTreeLds = 128 * 1024;      // bytes of the stages
-constexpr int kTreeBlock = 256;
 
-// 4 KiB from memory (uniform) into LDS (uniform), 4 x 16 bytes per lane, counted in vmcnt; off = 16 * lane.  In asm, so
-// that the compiler does not put a wait for it before every LDS read (it cannot tell the stages apart): the
+// n KiB (4 or 2) from memory (uniform) into LDS (uniform), n x 16 bytes per lane, counted in vmcnt; off = 16 * lane.  In
+// asm, so that the compiler does not put a wait for it before every LDS read (it cannot tell the stages apart): the
 // kernel waits itself (wait_vm).  No register is written.  The instructions' offsets count on both sides.
-__device__ __forceinline__ void load_to_lds(uint32_t lds, const uint16_t *src, uint32_t off) {
-  asm volatile(
-      "s_mov_b32 m0, %0\n\ts_nop 0\n\t"
-      "global_load_lds_dwordx4 %2, %1 nt\n\t"
-      "global_load_lds_dwordx4 %2, %1 offset:1024 nt\n\t"
-      "global_load_lds_dwordx4 %2, %1 offset:2048 nt\n\t"
-      "global_load_lds_dwordx4 %2, %1 offset:3072 nt" ::"s"(lds), "s"(src), "v"(off)
-      : "memory");
+template <int n> __device__ __forceinline__ void load_to_lds(uint32_t lds, const uint16_t *src, uint32_t off) {
+  if (n == 4)
+    asm volatile(
+        "s_mov_b32 m0, %0\n\ts_nop 0\n\t"
+        "global_load_lds_dwordx4 %2, %1 nt\n\t"
+        "global_load_lds_dwordx4 %2, %1 offset:1024 nt\n\t"
+        "global_load_lds_dwordx4 %2, %1 offset:2048 nt\n\t"
+        "global_load_lds_dwordx4 %2, %1 offset:3072 nt" ::"s"(lds), "s"(src), "v"(off)
+        : "memory");
+  else
+    asm volatile(
+        "s_mov_b32 m0, %0\n\ts_nop 0\n\t"
+        "global_load_lds_dwordx4 %2, %1 nt\n\t"
+        "global_load_lds_dwordx4 %2, %1 offset:1024 nt" ::"s"(lds), "s"(src), "v"(off)
+        : "memory");
 }
 // until at most n vector memory operations of this wave are under way (older ones complete first)
 template <int n> __device__ __forceinline__ void wait_vm() {
   asm volatile("s_waitcnt vmcnt(%0)" ::"n"(n) : "memory");
 }
 
+constexpr int tree_block(int HG) { return HG == 4 ? 256 : 512; }
+
 // HG: heads per workgroup
 template <int HG>
-__global__ __launch_bounds__(kTreeBlock) void tree_attn_kernel(AttnK a) {
-  constexpr int WPH = 4 / HG;                    // waves per head
+__global__ __launch_bounds__(tree_block(HG)) void tree_attn_kernel(AttnK a) {
+  constexpr int kBlock = tree_block(HG), kWaves = kBlock / 64;
+  constexpr int NT = HG == 4 ? 2 : 1;            // 32-row query tiles per wave
+  constexpr int WPH = kWaves / HG;               // waves per head
   constexpr int kStage = HG * 16384, kRing = kTreeLds / kStage;
-  constexpr int kLoads = 4 * HG;                 // loads per wave and stage
-  constexpr bool kEarly = HG < 4;                // K's operands are read a stage ahead
-  constexpr int kLater = kEarly ? kRing - 3 : 1;   // stages behind the awaited one that may be under way
+  constexpr int kLoads = kStage / 1024 / kWaves;   // loads per wave and stage
+  constexpr bool kShared = HG < 4;               // the waves read each other's loads
+  constexpr int kLater = kShared ? kRing - 2 : 1;  // stages behind the awaited one that may be under way
   __shared__ int scan_sh[16];
-  __shared__ int cum_sh[kTreeBlock + 1], m0_sh[kTreeBlock], bl_sh[kTreeBlock];
+  __shared__ int cum_sh[kBlock + 1], m0_sh[kBlock], bl_sh[kBlock];
   __shared__ int slot_sh[kAttnWinTiles];
   __shared__ int4 list_sh[kAttnWinTiles];        // the window's stages (struct Stage)
   // per stage K tiles [HG][2], then V tiles [HG][2], as they lie in the pool
@@ -62,18 +72,18 @@ __global__ __launch_bounds__(kTreeBlock) void tree_attn_kernel(AttnK a) {
   const int tid = threadIdx.x, lane = tid & 63, j = lane & 31, g = lane >> 5;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int part = blockIdx.x, kvh0 = blockIdx.y * HG, hw = w / WPH, kvh = kvh0 + hw;
-  const int rows = a.G * a.R, row0 = ((int)blockIdx.z * WPH + w % WPH) * 64;
+  const int rows = a.G * a.R, row0 = ((int)blockIdx.z * WPH + w % WPH) * 32 * NT;
   const bool wave_ok = kvh < a.n_kv && row0 < rows;    // other waves only bring tiles
   const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void *)stage_sh;
 
-  const bool one_chunk = a.B <= kTreeBlock, writer = part == 0 && blockIdx.y == 0 && blockIdx.z == 0;
+  const bool one_chunk = a.B <= kBlock, writer = part == 0 && blockIdx.y == 0 && blockIdx.z == 0;
   int TT = 0, T1 = 0, cb1 = 0, m1 = 0, r1 = 0;
   if (one_chunk) {
     T1 = tid < a.B ? seq_tiles(a, tid, m1, r1) : 0;
     cb1 = block_excl_scan(T1, scan_sh, &TT);
     if (writer && tid < a.B) a.cum[tid] = cb1;
   } else {
-    for (int c = 0; c < a.B; c += kTreeBlock) {
+    for (int c = 0; c < a.B; c += kBlock) {
       const int T = c + tid < a.B ? seq_tiles(a, c + tid, m1, r1) : 0;
       int tot;
       const int cb = TT + block_excl_scan(T, scan_sh, &tot);
@@ -87,9 +97,9 @@ __global__ __launch_bounds__(kTreeBlock) void tree_attn_kernel(AttnK a) {
   const int tpp = a.page_size >> 4;
 
   // this lane's queries: rows row0 + 32 t + j
-  int qi[2], qoff[2];
+  int qi[NT], qoff[NT];
 #pragma unroll
-  for (int t = 0; t < 2; ++t) {
+  for (int t = 0; t < NT; ++t) {
     const int r = row0 + 32 * t + j;
     qi[t] = r < rows && wave_ok ? r % a.R : -1;
     qoff[t] = qi[t] >= 0 ? (qi[t] * a.n_heads + kvh * a.G + r / a.R) * 128 : 0;
@@ -98,13 +108,13 @@ __global__ __launch_bounds__(kTreeBlock) void tree_attn_kernel(AttnK a) {
   int b = -1, m0 = 0, L = 0, cb = 0, seq_end = 0;
   bool dead = false;
   uint32_t wild = 0;
-  bf16x8_t qf[2][8];
-  unsigned long long anc[2];
-  bool node[2];
-  float m[2], l[2];
-  f32x16_t O[2][4];
+  bf16x8_t qf[NT][8];
+  unsigned long long anc[NT];
+  bool node[NT];
+  float m[NT], l[NT];
+  f32x16_t O[NT][4];
 
-  static_assert(kAttnWinTiles <= kTreeBlock, "a thread per tile of a window");
+  static_assert(kAttnWinTiles <= kBlock, "a thread per tile of a window");
   auto begin = [&](int c, int q) {
     b = c + q;
     m0 = __builtin_amdgcn_readfirstlane(m0_sh[q]);
@@ -116,7 +126,7 @@ __global__ __launch_bounds__(kTreeBlock) void tree_attn_kernel(AttnK a) {
     wild = 0;
     const uint16_t *qb = a.q + (long)b * a.R * a.n_heads * 128;
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
+    for (int t = 0; t < NT; ++t) {
       node[t] = qi[t] >= 0 && qi[t] < blen;
       anc[t] = node[t] ? a.masks[(long)b * a.R + qi[t]] : 0ull;
       if (blen < kMaxNodes) anc[t] &= (1ull << blen) - 1;
@@ -150,14 +160,14 @@ __global__ __launch_bounds__(kTreeBlock) void tree_attn_kernel(AttnK a) {
             const float f = bf16_to_f32(v[v_tile_off(tok & 15, 32 * c + 8 * (i >> 2) + 4 * g + (i & 3))]);
             if (!(fabsf(f) < INFINITY)) {
 #pragma unroll
-              for (int t = 0; t < 2; ++t)
+              for (int t = 0; t < NT; ++t)
                 if ((d < 0) | bool(anc[t] >> (d & 63) & 1)) O[t][c][i] += f;
             }
           }
       }
     }
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
+    for (int t = 0; t < NT; ++t) {
       const float lu = l[t] + __shfl_xor(l[t], 32, kWave);
       const int r = row0 + 32 * t + j;
       if (qi[t] < 0) continue;
@@ -188,22 +198,22 @@ __global__ __launch_bounds__(kTreeBlock) void tree_attn_kernel(AttnK a) {
     }
   };
 
-  bf16x8_t kf[8];         // K's operands of the stage to be computed
+  bf16x8_t kf[8];         // K's operands of a stage
   auto read_k = [&](const uint8_t *st) {
     const uint8_t *kt = st + hw * 8192 + (j >> 4) * 4096 + g * 256 + (j & 15) * 16;
 #pragma unroll
     for (int k = 0; k < 8; ++k) kf[k] = as_bf16x8(*reinterpret_cast<const uint4 *>(kt + k * 512));
   };
   // S[t][4 i + r]: the score of token 8 i + 4 g + r of the stage and query 32 t + j, unscaled
-  auto scores = [&](f32x16_t (&S)[2]) {
+  auto scores = [&](f32x16_t (&S)[NT]) {
 #pragma unroll
-    for (int t = 0; t < 2; ++t)
+    for (int t = 0; t < NT; ++t)
 #pragma unroll
       for (int i = 0; i < 16; ++i) S[t][i] = 0.f;
 #pragma unroll
     for (int k = 0; k < 8; ++k)
 #pragma unroll
-      for (int t = 0; t < 2; ++t) S[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[k], qf[t][k], S[t], 0, 0, 0);
+      for (int t = 0; t < NT; ++t) S[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[k], qf[t][k], S[t], 0, 0, 0);
   };
   uint4 vf[2][4];         // V's: tokens 4 g .. + 3 and 8 + 4 g .. + 3 of tile k, channel 32 c + j
   auto read_v = [&](const uint8_t *st) {
@@ -218,7 +228,7 @@ __global__ __launch_bounds__(kTreeBlock) void tree_attn_kernel(AttnK a) {
       }
   };
   // The masks of the tokens tb .. tb + 31, of which those below lim are there, and the rows' maxima brought up to date.
-  auto settle = [&](f32x16_t (&S)[2], int tb, int lim, bool mask) {
+  auto settle = [&](f32x16_t (&S)[NT], int tb, int lim, bool mask) {
     if (mask) {
       // entries past the last node are nothing; nodes' values that are inf or NaN are kept for the end (finish)
 #pragma unroll
@@ -241,9 +251,9 @@ __global__ __launch_bounds__(kTreeBlock) void tree_attn_kernel(AttnK a) {
         if (nodes && __any(mine)) wild |= 1u << (tb / 16 + k - m0 / 16);
       }
     }
-    float tmax[2];
+    float tmax[NT];
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
+    for (int t = 0; t < NT; ++t) {
       if (mask) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
@@ -260,7 +270,7 @@ __global__ __launch_bounds__(kTreeBlock) void tree_attn_kernel(AttnK a) {
       tmax[t] = fmaxf(x0, __shfl_xor(x0, 32, kWave)) * a.scale_log2;
     }
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
+    for (int t = 0; t < NT; ++t) {
       const bool up = tmax[t] > m[t] + kLazyLog2;
       if (__any(up)) {
         const float mn = up ? fmaxf(m[t], tmax[t]) : m[t];
@@ -274,9 +284,9 @@ __global__ __launch_bounds__(kTreeBlock) void tree_attn_kernel(AttnK a) {
   };
   // O += P V; the weights of query tile 1 are computed while the products of tile 0 run, six vector instructions
   // behind each
-  auto weigh = [&](f32x16_t (&S)[2]) {
+  auto weigh = [&](f32x16_t (&S)[NT]) {
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
+    for (int t = 0; t < NT; ++t) {
       const float ref = m[t] == -INFINITY ? 0.f : m[t];     // (a row that has seen nothing: every score is -inf)
       bf16x8_t hi[2], lo[2];
 #pragma unroll
@@ -302,9 +312,9 @@ __global__ __launch_bounds__(kTreeBlock) void tree_attn_kernel(AttnK a) {
         for (int c = 0; c < 4; ++c) O[t][c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(vf[k][c]), lo[k], O[t][c], 0, 0, 0);
       }
     }
-    __builtin_amdgcn_sched_group_barrier(0x402, 100, 0);
+    if (NT > 1) __builtin_amdgcn_sched_group_barrier(0x402, 100, 0);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
+    for (int i = 0; i < 16 * (NT - 1); ++i) {
       __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
       __builtin_amdgcn_sched_group_barrier(0x402, 6, 0);
     }
@@ -325,13 +335,15 @@ __global__ __launch_bounds__(kTreeBlock) void tree_attn_kernel(AttnK a) {
   };
   const uint32_t off = lane * 16;
   auto fetch = [&](const Stage &f, int p) {
+    // this wave's units of 4 KiB: K and V, both tiles, of its own head (HG = 4); one unit (2); half a unit (1)
 #pragma unroll
-    for (int q = 0; q < HG; ++q) {
-      // this wave's unit of 4 KiB: of its own head (HG = 4), else of units w HG + q: K or V, head, tile
-      const int u = HG == 4 ? (q >> 1) * 8 + hw * 2 + (q & 1) : w * HG + q;
+    for (int q = 0; q < (HG == 4 ? 4 : 1); ++q) {
+      const int u = HG == 4 ? (q >> 1) * 8 + hw * 2 + (q & 1) : HG == 2 ? w : w >> 1;
       const int h = (u >> 1) % HG, kv = u / (2 * HG), head = min(kvh0 + h, a.n_kv - 1);
       const uint16_t *src = (kv ? a.vp : a.kp) + (long)head * a.page_size * 128 + (long)(f.slot0 + (u & 1) * (f.slot1 - f.slot0)) * 2048;
-      load_to_lds(lds0 + p * kStage + u * 4096, src, off);
+      const uint32_t dst = lds0 + p * kStage + u * 4096;
+      if (HG > 1) load_to_lds<4>(dst, src, off);
+      else load_to_lds<2>(dst + (w & 1) * 2048, src + (w & 1) * 1024, off);
     }
   };
   // until a stage has arrived, with `later` stages fetched behind it (the window's last ones arrive together)
@@ -341,7 +353,7 @@ __global__ __launch_bounds__(kTreeBlock) void tree_attn_kernel(AttnK a) {
   };
 
   int run = 0;
-  for (int c = 0; c < a.B; c += kTreeBlock) {
+  for (int c = 0; c < a.B; c += kBlock) {
     int T, cbt, tot;
     if (one_chunk) {
       T = T1;
@@ -357,7 +369,7 @@ __global__ __launch_bounds__(kTreeBlock) void tree_attn_kernel(AttnK a) {
     if (cbeg >= e) break;
     __syncthreads();
     cum_sh[tid] = cbt;
-    if (tid == 0) cum_sh[kTreeBlock] = cend;
+    if (tid == 0) cum_sh[kBlock] = cend;
     m0_sh[tid] = m1;
     bl_sh[tid] = r1;
     const int xe = min(e, cend);
@@ -365,8 +377,8 @@ __global__ __launch_bounds__(kTreeBlock) void tree_attn_kernel(AttnK a) {
       const int nt = min(kAttnWinTiles, xe - x0);
       __syncthreads();
       int seq = 0;
-      for (int i = tid; i < nt; i += kTreeBlock) {      // (at most one turn)
-        int lo = 0, hi = min(kTreeBlock, a.B - c);
+      for (int i = tid; i < nt; i += kBlock) {      // (at most one turn)
+        int lo = 0, hi = min(kBlock, a.B - c);
         while (hi - lo > 1) {
           const int mid = (lo + hi) >> 1;
           if (cum_sh[mid] <= x0 + i) lo = mid;
@@ -394,38 +406,31 @@ __global__ __launch_bounds__(kTreeBlock) void tree_attn_kernel(AttnK a) {
       __syncthreads();
       // Stage f lies in place f % kRing.  `next` is the next one to fetch: kFetch of them before the first is computed,
       // then one per stage.
-      constexpr int kFetch = kEarly ? kRing - 1 : 2;
+      constexpr int kFetch = kShared ? kRing - 1 : 2;
       int next = min(kFetch, stages);
       for (int f = 0; f < next; ++f) fetch(stage(list_sh[f]), f);
       Stage cur = stage(list_sh[0]), ahead = stage(list_sh[min(next, stages - 1)]);
       auto fetch_next = [&]() {
         if (next < stages) fetch(ahead, next++ % kRing);
       };
-      if (kEarly) {
-        arrived(next - 1);
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
-        read_k(stage_sh);
-      }
       // (waves without rows compute along: what they hold is written nowhere)
       for (int k = 0; k < stages; ++k) {
-        arrived(next - 1 - (kEarly ? min(k + 1, stages - 1) : k));
+        arrived(next - 1 - k);
         const int4 cur_v = list_sh[min(k + 1, stages - 1)], ahead_v = list_sh[min(k + kFetch + 1, stages - 1)];
         const uint8_t *const st = stage_sh + k % kRing * kStage;
-        if (kEarly) {
+        if (kShared) {
           __builtin_amdgcn_s_barrier();
           asm volatile("" ::: "memory");
           fetch_next();
         }
         if (b != c + cur.seq) begin(c, cur.seq);
-        if (!kEarly) read_k(st);
+        read_k(st);
         __builtin_amdgcn_sched_barrier(0);
-        f32x16_t S[2];
+        f32x16_t S[NT];
         scores(S);
         read_v(st);
-        if (kEarly) read_k(stage_sh + (k + 1) % kRing * kStage);     // (behind the last stage: nothing that is used)
         __builtin_amdgcn_sched_barrier(0);
-        if (!kEarly) {
+        if (!kShared) {
           asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
           fetch_next();
         }
@@ -458,7 +463,7 @@ TreeGeom tree_geom(int rows, int n_kv) {
   g.rows_pad = g.wide ? (rows + 63) / 64 * 64 : g.rt * 16;
   if (!g.wide && g.heads_per_group > n_kv) g.heads_per_group = n_kv;
   g.groups = (n_kv + g.heads_per_group - 1) / g.heads_per_group;
-  g.block = g.wide ? kTreeBlock : 64 * g.heads_per_group;
+  g.block = g.wide ? 256 : 64 * g.heads_per_group;
   return g;
 }
 
@@ -481,7 +486,7 @@ template <int HG>
 void launch_wide(const AttnK &k, const TreeGeom &g, hipStream_t s) {
   static std::atomic<uint32_t> ready{0};
   reserve(tree_attn_kernel<HG>, kTreeLds, ready);
-  hipLaunchKernelGGL(tree_attn_kernel<HG>, dim3(k.parts, g.groups, g.row_groups), dim3(kTreeBlock), kTreeLds, s,
+  hipLaunchKernelGGL(tree_attn_kernel<HG>, dim3(k.parts, g.groups, g.row_groups), dim3(tree_block(HG)), kTreeLds, s,
                      k);
 }
 }  // namespace
