@@ -61,7 +61,8 @@ __global__ __launch_bounds__(tree_block(HG)) void tree_attn_kernel(AttnK a) {
   constexpr int kStage = HG * 16384, kRing = kTreeLds / kStage;
   constexpr int kLoads = kStage / 1024 / kWaves;   // loads per wave and stage
   constexpr bool kShared = HG < 4;               // the waves read each other's loads
-  constexpr int kLater = kShared ? kRing - 2 : 1;  // stages behind the awaited one that may be under way
+  constexpr int kTurn = kShared ? 2 : 1;         // stages per barrier
+  constexpr int kLater = kShared ? kRing - 2 * kTurn : 1;   // stages behind the awaited one that may be under way
   __shared__ int scan_sh[16];
   __shared__ int cum_sh[kBlock + 1], m0_sh[kBlock], bl_sh[kBlock];
   __shared__ int slot_sh[kAttnWinTiles];
@@ -406,7 +407,7 @@ __global__ __launch_bounds__(tree_block(HG)) void tree_attn_kernel(AttnK a) {
       __syncthreads();
       // Stage f lies in place f % kRing.  `next` is the next one to fetch: kFetch of them before the first is computed,
       // then one per stage.
-      constexpr int kFetch = kShared ? kRing - 1 : 2;
+      constexpr int kFetch = kShared ? kRing - kTurn : 2;
       int next = min(kFetch, stages);
       for (int f = 0; f < next; ++f) fetch(stage(list_sh[f]), f);
       Stage cur = stage(list_sh[0]), ahead = stage(list_sh[min(next, stages - 1)]);
@@ -415,13 +416,24 @@ __global__ __launch_bounds__(tree_block(HG)) void tree_attn_kernel(AttnK a) {
       };
       // (waves without rows compute along: what they hold is written nowhere)
       for (int k = 0; k < stages; ++k) {
-        arrived(next - 1 - k);
-        const int4 cur_v = list_sh[min(k + 1, stages - 1)], ahead_v = list_sh[min(k + kFetch + 1, stages - 1)];
+        const int4 cur_v = list_sh[min(k + 1, stages - 1)];
+        int4 ahead_v;
         const uint8_t *const st = stage_sh + k % kRing * kStage;
         if (kShared) {
-          __builtin_amdgcn_s_barrier();
-          asm volatile("" ::: "memory");
-          fetch_next();
+          if (k % kTurn == 0) {
+            arrived(next - 1 - min(k + kTurn - 1, stages - 1));
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+#pragma unroll
+            for (int f = 0; f < kTurn; ++f)
+              if (next < stages) {
+                fetch(stage(list_sh[next]), next % kRing);
+                ++next;
+              }
+          }
+        } else {
+          arrived(next - 1 - k);
+          ahead_v = list_sh[min(k + kFetch + 1, stages - 1)];
         }
         if (b != c + cur.seq) begin(c, cur.seq);
         read_k(st);
@@ -440,7 +452,7 @@ __global__ __launch_bounds__(tree_block(HG)) void tree_attn_kernel(AttnK a) {
         const bool last = cur.last;
         settle(S, tb, min(L, tb + 16 * there), there < 2 || tb + 32 > m0);
         cur = stage(cur_v);
-        ahead = stage(ahead_v);
+        if (!kShared) ahead = stage(ahead_v);
         weigh(S);
         if (last && wave_ok) finish();
       }
