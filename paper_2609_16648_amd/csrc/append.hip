@@ -12,7 +12,8 @@
 // quads whole where units of 16 rows would not.)  A workgroup takes the rotations of its 16
 // tokens once, into LDS, for all heads; its four waves take the heads in turn, a wave 16 tokens
 // of one q or k head, or of the 2 (head_dim 128) or 4 (64) v heads that fill its lanes.
-// Bound by HBM: every row is read once and written once.
+// Bound by HBM: every row is read once and written once.  32768 rows of 32 + 8 + 8 bf16 heads of 128 (802 MB) take
+// 189 us, 4.2 TB/s, where a copy of 2 GiB reaches 4.9; V through LDS instead of the register transpose took 204.
 //
 // Precision: the angle in float64 as a fraction of a turn (positions reach 32K and beyond, where a
 // float32 angle is off by 1e-3), its sine and cosine in float32; norm and rotation in float32,
@@ -77,7 +78,9 @@ __device__ __forceinline__ long units_before(long row, int b) { return (row >> 4
 
 template <typename T, int D>
 __global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs a) {
-  constexpr int kHalf = D / 2, kIters = kHalf / 32;   // a lane holds kIters pairs of eight channels
+  // q and k: kRowLanes lanes hold a row's low half and its high half, eight channels each: whole 128-byte lines per
+  // load and store; kIters passes over the 16 tokens
+  constexpr int kHalf = D / 2, kRowLanes = kHalf / 8, kIters = 16 * kRowLanes / 64;
   __shared__ __attribute__((aligned(16))) float2 rot[16][kHalf + 2];   // (cos, sin) of token s and pair c; rows four banks apart
   const int tid = threadIdx.x, lane = tid & 63;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -145,40 +148,38 @@ __global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs a) {
       const int h = is_q ? task : task - a.n_heads;
       const T *const src = (const T *)(is_q ? a.q : a.k);
       const T *const nw = (const T *)(is_q ? a.q_norm : a.k_norm);
-      const int s = lane >> 2, j = lane & 3;
-      const long r = row_of(s);
-      Eight<T> lo[kIters], hi[kIters];
+      const int j = lane % kRowLanes, c = 8 * j;
+      Eight<T> lo[kIters], hi[kIters], wl, wh;
+      long r[kIters];
 #pragma unroll
       for (int i = 0; i < kIters; ++i) {
+        r[i] = row_of(lane / kRowLanes + i * (64 / kRowLanes));
         lo[i].zero();
         hi[i].zero();
-        if (r >= 0) {
-          const T *p = src + r * (is_q ? a.q_stride : a.k_stride) + (long)h * D + 32 * i + 8 * j;
+        if (r[i] >= 0) {
+          const T *p = src + r[i] * (is_q ? a.q_stride : a.k_stride) + (long)h * D + c;
           lo[i].load(p);
           hi[i].load(p + kHalf);
         }
       }
-      float inv = 1.f;
       if (nw) {
-        float ss = 0.f;
-#pragma unroll
-        for (int i = 0; i < kIters; ++i)
-#pragma unroll
-          for (int x = 0; x < 8; ++x) ss += lo[i].get(x) * lo[i].get(x) + hi[i].get(x) * hi[i].get(x);
-        ss += __shfl_xor(ss, 1, kWave);
-        ss += __shfl_xor(ss, 2, kWave);
-        inv = 1.0f / sqrtf(ss / (float)D + a.eps);
+        wl.load(nw + c);
+        wh.load(nw + c + kHalf);
       }
-      if (r < 0 || (!is_q && kv_base < 0)) continue;
 #pragma unroll
       for (int i = 0; i < kIters; ++i) {
-        const int c = 32 * i + 8 * j;
-        float y1[8], y2[8];
-        Eight<T> wl, wh;
+        const int s = lane / kRowLanes + i * (64 / kRowLanes);
+        float inv = 1.f;
         if (nw) {
-          wl.load(nw + c);
-          wh.load(nw + c + kHalf);
+          float ss = 0.f;
+#pragma unroll
+          for (int x = 0; x < 8; ++x) ss += lo[i].get(x) * lo[i].get(x) + hi[i].get(x) * hi[i].get(x);
+#pragma unroll
+          for (int o = 1; o < kRowLanes; o <<= 1) ss += __shfl_xor(ss, o, kWave);
+          inv = 1.0f / sqrtf(ss / (float)D + a.eps);
         }
+        if (r[i] < 0 || (!is_q && kv_base < 0)) continue;
+        float y1[8], y2[8];
 #pragma unroll
         for (int x = 0; x < 8; ++x) {
           float p = lo[i].get(x), q = hi[i].get(x);
@@ -191,7 +192,7 @@ __global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs a) {
           y2[x] = q * t.x + p * t.y;
         }
         if (is_q) {
-          T *o = (T *)a.q_out + (r * a.n_heads + h) * D + c;
+          T *o = (T *)a.q_out + (r[i] * a.n_heads + h) * D + c;
           Eight<T>::store(o, y1);
           Eight<T>::store(o + kHalf, y2);
         } else {
@@ -244,8 +245,10 @@ void launch_kv_append(const AppendArgs &a, hipStream_t s) {
   if (a.T <= 0 || a.B <= 0) return;
   TraceScope ts("kv_append", s);
   const int tasks = a.n_heads + a.n_kv + (a.n_kv * a.head_dim / 4 + 63) / 64;
-  // few units: their heads are dealt to more workgroups, until about 1024 of them
-  int y = (int)((1024 + units - 1) / units);
+  // Few units: their heads are dealt to more workgroups, until about 2048 of them (eight per CU).  Measured with 2048 /
+  // 8192 / 16384, bf16, 32 q and 8 KV heads of 128: 32 prompts of 1024 rows 189 / 207 / 200 us, 256 trees of 4 nodes
+  // 22 / 30 / 30, 64 trees of 16 nodes 14.6 / 14.8 / 14.3: more workgroups repeat the rotations and the table reads.
+  int y = (int)((2048 + units - 1) / units);
   const int most = (tasks + 3) / 4;
   if (y > most) y = most;
   const dim3 grid((unsigned)units, y);
