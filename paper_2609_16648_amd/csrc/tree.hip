@@ -1,5 +1,7 @@
 // Draft trees: the masks of a batch of trees, the accept walk, and the commit of the accepted
 // path.  A tree has at most 64 nodes: a wave holds one sequence's, a node per lane.
+#include <type_traits>
+
 #include "common.h"
 #include "tree.h"
 
@@ -77,7 +79,7 @@ __global__ __launch_bounds__(256) void tree_accept_kernel(int B, int N, const in
   if (i == 0) n_accept[b] = n > 0 ? steps : -1;
 }
 
-constexpr int kCommitLayers = 32;    // layers per launch (their pool bases are kernel arguments)
+constexpr int kCommitLayers = 128;   // layers per launch (their pool bases are kernel arguments, 2 KiB of 4)
 struct CommitArgs {
   void *pools[kCommitLayers][2];
   const int32_t *path, *n_accept, *block_table, *seq_lens;
@@ -85,24 +87,27 @@ struct CommitArgs {
   int N, n_kv, page_size, max_pages, num_pages, layers, report;
 };
 
-// One workgroup per (sequence, layer, K or V).  A thread owns the same channels of every token (a
-// 16-byte piece of K, one element of V), and moves the path's entries in increasing order, the
-// loads of a batch before its stores.  That order is enough: entry i moves from slot path[i] >= i
-// to slot i, so no earlier move has written what it reads, and a later one that overwrites slot
-// path[i] comes behind it in the same thread.
-// Bound by latency (table, lengths, entries: three dependent loads), then by the lines touched: a
-// token's K lies in 16-byte pieces and its V in single elements.
+// One workgroup per (sequence, layer, K or V).  A thread owns the same pieces of every token (16 bytes of K, one element
+// of V), and moves the path's entries in increasing order, the loads of a batch before its stores.  That order is
+// enough: entry i moves from slot path[i] >= i to slot i, so no earlier move has written what it reads, and a later
+// one that overwrites slot path[i] comes behind it in the same thread.
+// Bound by latency: two dependent loads for the places, then a batch of kBatch entries of kWide pieces each in one
+// round trip (a token's K lies in 16-byte pieces and its V in single elements), and then by the lines that those touch.
+// 64 sequences, 36 layers of 8 bf16 heads of 128: 37 us in one launch (60 in two, with batches of four elements);
+// one sequence 8.
 template <typename E, int D>
 __global__ __launch_bounds__(256) void tree_commit_kernel(CommitArgs a) {
-  __shared__ long src_sh[kMaxNodes], dst_sh[kMaxNodes];    // element offsets of (page, tile) blocks, -1: stays
+  __shared__ long src_sh[kMaxNodes], dst_sh[kMaxNodes];    // element offsets of (page, tile) blocks
   __shared__ int ss_sh[kMaxNodes], ds_sh[kMaxNodes];       // token in the tile
   __shared__ int count_sh;
   const int b = blockIdx.x, tid = threadIdx.x;
-  int n = a.n_accept[b];
-  n = n < -1 ? -1 : (n >= a.N ? a.N - 1 : n);
   if (tid < 64) {
     const int i = tid;
-    const int p = i <= n ? a.path[(long)b * a.N + i] : -1;
+    const int p_any = i < a.N ? a.path[(long)b * a.N + i] : -1;
+    const long m = a.seq_lens[b];
+    int n = a.n_accept[b];
+    n = n < -1 ? -1 : (n >= a.N ? a.N - 1 : n);
+    const int p = i <= n ? p_any : -1;
     const int before = __shfl_up(p, 1, kWave);
     const bool bad = i <= n && (p < i || p >= a.N || (i > 0 && p <= before));
     const bool any_bad = __any(bad);
@@ -111,19 +116,20 @@ __global__ __launch_bounds__(256) void tree_commit_kernel(CommitArgs a) {
     long src = 0, dst = 0;
     int ss = 0, ds = 0;
     if (moves) {
-      auto place = [&](long slot, long &base, int &s) -> bool {
-        const long pi = slot / a.page_size;
-        const int page = slot >= 0 && pi < a.max_pages ? a.block_table[(long)b * a.max_pages + pi] : -1;
-        if (page < 0 || page >= a.num_pages) return false;
-        const int off = (int)(slot % a.page_size);
-        base = (long)page * a.n_kv * a.page_size * D + (long)(off & ~15) * D;
-        s = off & 15;
-        return true;
-      };
-      const long m = a.seq_lens[b];
-      if (!place(m + p, src, ss) || !place(m + i, dst, ds)) {
+      // the pages of both places are asked for together
+      const long from = m + p, to = m + i, pf = from / a.page_size, pt = to / a.page_size;
+      const bool in = m >= 0 && pf < a.max_pages;           // (to < from)
+      const int32_t *bt = a.block_table + (long)b * a.max_pages;
+      const int gf = in ? bt[pf] : -1, gt = in ? bt[pt] : -1;
+      if (gf < 0 || gf >= a.num_pages || gt < 0 || gt >= a.num_pages) {
         moves = false;
         if (a.report) raise_dev_err(a.dev_err, GM_DEVERR_PAGE);
+      } else {
+        const int of = (int)(from % a.page_size), ot = (int)(to % a.page_size);
+        src = (long)gf * a.n_kv * a.page_size * D + (long)(of & ~15) * D;
+        dst = (long)gt * a.n_kv * a.page_size * D + (long)(ot & ~15) * D;
+        ss = of & 15;
+        ds = ot & 15;
       }
     }
     const unsigned long long live = __ballot(moves);
@@ -138,46 +144,43 @@ __global__ __launch_bounds__(256) void tree_commit_kernel(CommitArgs a) {
   }
   __syncthreads();
   const int count = count_sh;
-  constexpr int kBatch = 4;
+  if (count == 0) return;
+  // `pieces` of P, kWide per thread at a time; place(piece, token) is a piece's element offset behind its head's tile
+  auto move = [&](auto *pool, int pieces, auto wide, auto batch, auto head_of, auto place) {
+    constexpr int kWide = decltype(wide)::value, kBatch = decltype(batch)::value;
+    using P = typename std::remove_pointer<decltype(pool)>::type;
+    for (int x0 = tid; x0 < pieces; x0 += 256 * kWide) {
+      for (int i0 = 0; i0 < count; i0 += kBatch) {
+        P v[kBatch][kWide];
+#pragma unroll
+        for (int e = 0; e < kBatch; ++e)
+#pragma unroll
+          for (int u = 0; u < kWide; ++u) {
+            const int x = x0 + 256 * u;
+            if (i0 + e < count && x < pieces) v[e][u] = *place(pool, src_sh[i0 + e] + head_of(x), x, ss_sh[i0 + e]);
+          }
+#pragma unroll
+        for (int e = 0; e < kBatch; ++e)
+#pragma unroll
+          for (int u = 0; u < kWide; ++u) {
+            const int x = x0 + 256 * u;
+            if (i0 + e < count && x < pieces) *place(pool, dst_sh[i0 + e] + head_of(x), x, ds_sh[i0 + e]) = v[e][u];
+          }
+      }
+    }
+  };
+  const long head = (long)a.page_size * D;
   if (blockIdx.z == 0) {
-    // K: pieces of eight channels
-    constexpr int kPieces = D / 8;
-    E *const pool = (E *)a.pools[blockIdx.y][0];
-    for (int x = tid; x < a.n_kv * kPieces; x += 256) {
-      const long head = (long)(x / kPieces) * a.page_size * D;
-      const int c = x % kPieces * 8;
-      for (int i0 = 0; i0 < count; i0 += kBatch) {
-        constexpr int kWords = 8 * sizeof(E) / 16;
-        uint4 v[kBatch][kWords];
-#pragma unroll
-        for (int e = 0; e < kBatch; ++e)
-          if (i0 + e < count)
-#pragma unroll
-            for (int q = 0; q < kWords; ++q)
-              v[e][q] = reinterpret_cast<const uint4 *>(pool + src_sh[i0 + e] + head + k_tile_off(ss_sh[i0 + e], c))[q];
-#pragma unroll
-        for (int e = 0; e < kBatch; ++e)
-          if (i0 + e < count)
-#pragma unroll
-            for (int q = 0; q < kWords; ++q)
-              reinterpret_cast<uint4 *>(pool + dst_sh[i0 + e] + head + k_tile_off(ds_sh[i0 + e], c))[q] = v[e][q];
-      }
-    }
+    constexpr int kElems = 16 / sizeof(E), kPieces = D / kElems;
+    move((uint4 *)a.pools[blockIdx.y][0], a.n_kv * kPieces, std::integral_constant<int, 1>{},
+         std::integral_constant<int, 8>{}, [&](int x) { return x / kPieces * head; },
+         [&](uint4 *pool, long base, int x, int s) {
+           return (uint4 *)((E *)pool + base + k_tile_off(s, x % kPieces * kElems));
+         });
   } else {
-    E *const pool = (E *)a.pools[blockIdx.y][1];
-    for (int x = tid; x < a.n_kv * D; x += 256) {
-      const long head = (long)(x / D) * a.page_size * D;
-      const int c = x % D;
-      for (int i0 = 0; i0 < count; i0 += kBatch) {
-        E v[kBatch];
-#pragma unroll
-        for (int e = 0; e < kBatch; ++e)
-          if (i0 + e < count) v[e] = pool[src_sh[i0 + e] + head + v_tile_off(ss_sh[i0 + e], c)];
-#pragma unroll
-        for (int e = 0; e < kBatch; ++e)
-          if (i0 + e < count) pool[dst_sh[i0 + e] + head + v_tile_off(ds_sh[i0 + e], c)] = v[e];
-      }
-    }
+    move((E *)a.pools[blockIdx.y][1], a.n_kv * D, std::integral_constant<int, 4>{}, std::integral_constant<int, 4>{},
+         [&](int x) { return x / D * head; },
+         [&](E *pool, long base, int x, int s) { return pool + base + v_tile_off(s, x % D); });
   }
 }
 
