@@ -423,7 +423,8 @@ extern "C" gm_status gm_kv_append(const gm_model_config *cfg, const gm_kv_cache 
                                   void *stream) {
   gm_status st = check_config(cfg, B, 0);
   if (st != GM_OK) return st;
-  if (T < 0 || max_rows < 0 || max_rows > T) return fail(GM_ERR_INVALID_ARG, "bad T=%d max_rows=%d", T, max_rows);
+  if (T < 0 || max_rows < 0) return fail(GM_ERR_INVALID_ARG, "bad T=%d max_rows=%d", T, max_rows);
+  if (max_rows > T) max_rows = T;
   if (T > kMaxAppendRows || B > kMaxTrees)
     return fail(GM_ERR_UNSUPPORTED, "%d rows of %d sequences exceed %d of %d", T, B, kMaxAppendRows, kMaxTrees);
   if (!cache) return fail(GM_ERR_INVALID_ARG, "null cache");

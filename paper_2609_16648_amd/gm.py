@@ -157,16 +157,34 @@ def _ptr(t: Optional[torch.Tensor]):
         return None
     if not t.is_contiguous():
         raise ValueError("tensors passed to libgm must be contiguous")
-    return ctypes.c_void_p(t.data_ptr())
+    return t.data_ptr()
 
 
-def _stream(stream) -> ctypes.c_void_p:
-    s = torch.cuda.current_stream() if stream is None else stream
-    return ctypes.c_void_p(s.cuda_stream)
+# a stream's handle without building a torch Stream for it (0.1 us against 3 per call), where torch offers it
+_current_handle = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
+def _stream(stream) -> int:
+    if stream is not None:
+        return stream.cuda_stream
+    if _current_handle is not None:
+        return _current_handle(torch.cuda.current_device())
+    return torch.cuda.current_stream().cuda_stream
+
+
+def _here(stream, *tensors) -> int:
+    """The stream's handle, once it and every tensor are known to be on the current device, which the kernels run on."""
+    dev = torch.cuda.current_device()
+    if stream is not None and stream.device_index != dev:
+        raise ValueError("a stream of device %d, the current device is %d" % (stream.device_index, dev))
+    for t in tensors:
+        if t is not None and t.get_device() != dev:
+            raise ValueError("a tensor on %s, the current device is %d" % (t.device, dev))
+    return _stream(stream)
 
 
 def _need(t: torch.Tensor, dtype, shape, name: str):
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape):
+    if t.dtype != dtype or t.shape != tuple(shape):
         raise ValueError("%s: expected %s %s, got %s %s" % (name, dtype, tuple(shape), t.dtype, tuple(t.shape)))
     if not t.is_cuda:
         raise ValueError("%s must be a device tensor" % name)
@@ -558,7 +576,7 @@ def _rows(t: torch.Tensor, dtype, heads: int, dim: int, rows: int, name: str):
         raise ValueError("%s must be a device tensor" % name)
     if (dim > 1 and t.stride(2) != 1) or (heads > 1 and t.stride(1) != dim) or (rows > 1 and t.stride(0) < heads * dim):
         raise ValueError("%s: the heads of a row must be contiguous and the rows apart" % name)
-    return c_void_p(t.data_ptr()), t.stride(0) if rows > 1 else heads * dim
+    return t.data_ptr(), t.stride(0) if rows > 1 else heads * dim
 
 
 def kv_append(cfg: ModelConfig, cache: PagedCache, layer: int, k: torch.Tensor, v: torch.Tensor,
@@ -591,7 +609,7 @@ def kv_append(cfg: ModelConfig, cache: PagedCache, layer: int, k: torch.Tensor, 
     cs = cache.struct()
     _check(lib().gm_kv_append(ctypes.byref(cfg), ctypes.byref(cs), layer, B, T, max_rows, _ptr(row_start),
                               _ptr(offsets), pq, sq, pk, sk, pv, sv, _ptr(q_norm), _ptr(k_norm), _ptr(q_out),
-                              _ptr(dev_err), _stream(stream)))
+                              _ptr(dev_err), _here(stream, q, k, v, q_out, row_start, offsets, q_norm, k_norm, dev_err, cache.seq_lens, cache.k[0])))
 
 
 def tree_masks(parents: torch.Tensor, masks: torch.Tensor, depths: torch.Tensor,
@@ -604,7 +622,7 @@ def tree_masks(parents: torch.Tensor, masks: torch.Tensor, depths: torch.Tensor,
     if n_nodes is not None:
         _need(n_nodes, torch.int32, (B,), "n_nodes")
     _check(lib().gm_tree_masks(B, N, _ptr(parents), _ptr(n_nodes), _ptr(masks), _ptr(depths), _ptr(dev_err),
-                               _stream(stream)))
+                               _here(stream, parents, n_nodes, masks, depths, dev_err)))
 
 
 def tree_attention(cfg: ModelConfig, cache: PagedCache, layer: int, q: torch.Tensor, masks: torch.Tensor,
@@ -621,7 +639,7 @@ def tree_attention(cfg: ModelConfig, cache: PagedCache, layer: int, q: torch.Ten
     cs = cache.struct()
     buf = ws.get(workspace_size(GM_OP_TREE_ATTENTION, cfg, B, N, cache.max_ctx))
     _check(lib().gm_tree_attention(ctypes.byref(cfg), ctypes.byref(cs), layer, B, N, _ptr(q), _ptr(masks),
-                                   _ptr(n_nodes), _ptr(out), _ptr(buf), buf.numel(), _ptr(dev_err), _stream(stream)))
+                                   _ptr(n_nodes), _ptr(out), _ptr(buf), buf.numel(), _ptr(dev_err), _here(stream, q, masks, n_nodes, out, buf, dev_err, cache.seq_lens, cache.k[0])))
 
 
 def tree_accept(parents: torch.Tensor, tokens: torch.Tensor, next_ids: torch.Tensor, path: torch.Tensor,
@@ -636,7 +654,7 @@ def tree_accept(parents: torch.Tensor, tokens: torch.Tensor, next_ids: torch.Ten
     if n_nodes is not None:
         _need(n_nodes, torch.int32, (B,), "n_nodes")
     _check(lib().gm_tree_accept(B, N, _ptr(parents), _ptr(tokens), _ptr(next_ids), _ptr(n_nodes), _ptr(path),
-                                _ptr(n_accept), _ptr(out_tokens), _stream(stream)))
+                                _ptr(n_accept), _ptr(out_tokens), _here(stream, parents, tokens, next_ids, n_nodes, path, n_accept, out_tokens)))
 
 
 def tree_commit(cfg: ModelConfig, cache: PagedCache, path: torch.Tensor, n_accept: torch.Tensor,
@@ -649,7 +667,7 @@ def tree_commit(cfg: ModelConfig, cache: PagedCache, path: torch.Tensor, n_accep
         _need(committed_slots, torch.int32, (B, N), "committed_slots")
     cs = cache.struct()
     _check(lib().gm_tree_commit(ctypes.byref(cfg), ctypes.byref(cs), B, N, _ptr(path), _ptr(n_accept),
-                                _ptr(committed_slots), _ptr(dev_err), _stream(stream)))
+                                _ptr(committed_slots), _ptr(dev_err), _here(stream, path, n_accept, committed_slots, dev_err, cache.seq_lens, cache.k[0])))
 
 
 # ------------------------------------------------------------------------ token log-probabilities
@@ -662,7 +680,7 @@ def _logit_rows(t: torch.Tensor, name: str):
     M, V = t.shape
     if (V > 1 and t.stride(1) != 1) or (M > 1 and t.stride(0) < V):
         raise ValueError("%s: the ids of a row must be contiguous and the rows apart" % name)
-    return c_void_p(t.data_ptr()), GM_BF16 if t.dtype == torch.bfloat16 else GM_F32, t.stride(0) if M > 1 else V
+    return t.data_ptr(), GM_BF16 if t.dtype == torch.bfloat16 else GM_F32, t.stride(0) if M > 1 else V
 
 
 def token_logprobs(logits: torch.Tensor, ids: Optional[torch.Tensor], ws: Workspace,
@@ -691,7 +709,7 @@ def token_logprobs(logits: torch.Tensor, ids: Optional[torch.Tensor], ws: Worksp
     buf = ws.get(workspace_size(GM_OP_TOKEN_LOGPROBS, cfg, M, topk, 0))
     _check(lib().gm_token_logprobs(M, V, dt, pz, ld, temperature, _ptr(ids), _ptr(logp), _ptr(entropy), topk,
                                    _ptr(top_logp), _ptr(top_ids), _ptr(stats), _ptr(buf), buf.numel(), _ptr(dev_err),
-                                   _stream(stream)))
+                                   _here(stream, logits, ids, logp, entropy, top_logp, top_ids, stats, buf, dev_err)))
 
 
 def token_logprobs_grad(logits: torch.Tensor, ids: Optional[torch.Tensor], stats: torch.Tensor,
@@ -710,7 +728,7 @@ def token_logprobs_grad(logits: torch.Tensor, ids: Optional[torch.Tensor], stats
         if t is not None:
             _need(t, torch.float32, (M,), name)
     _check(lib().gm_token_logprobs_grad(M, V, dt, pz, ld, temperature, _ptr(ids), _ptr(stats), _ptr(entropy),
-                                        _ptr(g_logp), _ptr(g_entropy), pg, ldg, _stream(stream)))
+                                        _ptr(g_logp), _ptr(g_entropy), pg, ldg, _here(stream, logits, ids, stats, entropy, g_logp, g_entropy, grad)))
 
 
 # ------------------------------------------------------------------------ kernel timing

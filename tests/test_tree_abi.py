@@ -40,8 +40,10 @@ def test_kv_append_rejects():
     assert _append(cache=_cache(page_size=24)) == U
     assert _append(cache=_cache(table=None)) == A
     assert _append(T=30) == A and _append(max_rows=7) == A                # not B equal shares; shares of 8
-    assert _append(max_rows=33) == A and _append(T=-1) == A and _append(B=-1) == A
-    assert _append(row_start=FAKE, T=31, max_rows=200, cache=_cache(max_ctx=0)) == A
+    assert _append(max_rows=-1) == A and _append(T=-1) == A and _append(B=-1) == A
+    # a bound above the rows that there are counts as those (129 + 31 fit in 160, 130 + 31 do not)
+    assert _append(row_start=FAKE, T=31, max_rows=200, cache=_cache(max_ctx=130)) == C
+    assert _append(row_start=FAKE, T=31, max_rows=200, cache=_cache(max_ctx=129), k=None) == A
     assert _append(T=(1 << 27) + 4, max_rows=8, row_start=FAKE) == U
     assert _append(k=None) == A and _append(v=None) == A
     assert _append(q=None) == A and _append(qo=None) == A and "together" in gm.last_error()
@@ -143,3 +145,14 @@ def test_binding_rejects_host_tensors_and_shapes():
         gm.token_logprobs(t(2, 4, dtype=torch.float16), None, None)
     with pytest.raises(ValueError, match="device tensor"):
         gm.token_logprobs(t(2, 4), None, None)
+
+
+def test_binding_takes_the_current_device_only(monkeypatch):
+    on = lambda d: type("T", (), dict(get_device=lambda self: d, device="cuda:%d" % d))()  # noqa: E731
+    stream = lambda d: type("S", (), dict(device_index=d, cuda_stream=77))()  # noqa: E731
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    assert gm._here(stream(1), on(1), None, on(1)) == 77
+    with pytest.raises(ValueError, match="the current device is 1"):
+        gm._here(stream(1), on(1), on(0))
+    with pytest.raises(ValueError, match="a stream of device 0"):
+        gm._here(stream(0), on(1))
