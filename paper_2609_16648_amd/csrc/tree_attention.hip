@@ -65,8 +65,9 @@ __global__ __launch_bounds__(tree_block(HG)) void tree_attn_kernel(AttnK a) {
   constexpr int kLater = kShared ? kRing - 2 * kTurn : 1;   // stages behind the awaited one that may be under way
   __shared__ int scan_sh[16];
   __shared__ int cum_sh[kBlock + 1], m0_sh[kBlock], bl_sh[kBlock];
-  __shared__ int slot_sh[kAttnWinTiles];
-  __shared__ int4 list_sh[kAttnWinTiles];        // the window's stages (struct Stage)
+  constexpr int kWin = kBlock;                   // tiles per window
+  __shared__ int slot_sh[kWin];
+  __shared__ int4 list_sh[kWin];                 // the window's stages (struct Stage)
   // per stage K tiles [HG][2], then V tiles [HG][2], as they lie in the pool
   extern __shared__ __attribute__((aligned(16))) uint8_t stage_sh[];
 
@@ -115,7 +116,6 @@ __global__ __launch_bounds__(tree_block(HG)) void tree_attn_kernel(AttnK a) {
   float m[NT], l[NT];
   f32x16_t O[NT][4];
 
-  static_assert(kAttnWinTiles <= kBlock, "a thread per tile of a window");
   auto begin = [&](int c, int q) {
     b = c + q;
     m0 = __builtin_amdgcn_readfirstlane(m0_sh[q]);
@@ -268,7 +268,9 @@ __global__ __launch_bounds__(tree_block(HG)) void tree_attn_kernel(AttnK a) {
       float x0 = __builtin_amdgcn_fmed3f(S[t][0], S[t][1], INFINITY);
 #pragma unroll
       for (int i = 2; i < 16; i += 2) x0 = fmaxf(x0, __builtin_amdgcn_fmed3f(S[t][i], S[t][i + 1], INFINITY));
-      tmax[t] = fmaxf(x0, __shfl_xor(x0, 32, kWave)) * a.scale_log2;
+      // (the other half of the wave holds the row's other tokens)
+      const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(x0), __float_as_uint(x0), false, false);
+      tmax[t] = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1])) * a.scale_log2;
     }
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
@@ -331,8 +333,8 @@ __global__ __launch_bounds__(tree_block(HG)) void tree_attn_kernel(AttnK a) {
   auto stage = [&](const int4 &v) {
     const int meta = __builtin_amdgcn_readfirstlane(v.z);
     return Stage{__builtin_amdgcn_readfirstlane(v.x), __builtin_amdgcn_readfirstlane(v.y),
-                 __builtin_amdgcn_readfirstlane(v.w), meta & 255, meta >> 8 & 3, (meta >> 10 & 1) != 0,
-                 (meta >> 11 & 1) != 0};
+                 __builtin_amdgcn_readfirstlane(v.w), meta & 0xffff, meta >> 16 & 3, (meta >> 18 & 1) != 0,
+                 (meta >> 19 & 1) != 0};
   };
   const uint32_t off = lane * 16;
   auto fetch = [&](const Stage &f, int p) {
@@ -374,11 +376,11 @@ __global__ __launch_bounds__(tree_block(HG)) void tree_attn_kernel(AttnK a) {
     m0_sh[tid] = m1;
     bl_sh[tid] = r1;
     const int xe = min(e, cend);
-    for (int x0 = max(s, cbeg); x0 < xe; x0 += kAttnWinTiles) {
-      const int nt = min(kAttnWinTiles, xe - x0);
+    for (int x0 = max(s, cbeg); x0 < xe; x0 += kWin) {
+      const int nt = min(kWin, xe - x0);
       __syncthreads();
       int seq = 0;
-      for (int i = tid; i < nt; i += kBlock) {      // (at most one turn)
+      if (const int i = tid; i < nt) {              // a thread per tile
         int lo = 0, hi = min(kBlock, a.B - c);
         while (hi - lo > 1) {
           const int mid = (lo + hi) >> 1;
@@ -402,7 +404,7 @@ __global__ __launch_bounds__(tree_block(HG)) void tree_attn_kernel(AttnK a) {
         const int s0 = slot_sh[tid], s1 = n > 1 ? slot_sh[tid + 1] : s0;
         const int there = s0 < 0 ? 0 : s1 < 0 ? 1 : n;
         const bool last = x + n == min(e, cum_sh[seq + 1]);
-        list_sh[at] = make_int4(max(s0, 0), max(s1, 0), seq | there << 8 | (there < n) << 10 | last << 11, x);
+        list_sh[at] = make_int4(max(s0, 0), max(s1, 0), seq | there << 16 | (there < n) << 18 | last << 19, x);
       }
       __syncthreads();
       // Stage f lies in place f % kRing.  `next` is the next one to fetch: kFetch of them before the first is computed,

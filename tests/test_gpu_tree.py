@@ -18,7 +18,7 @@ import torch
 import synth
 from helpers import need_gpu, t32, i32
 from oracle import tree as otree
-from paper_2609_16648_amd import gm
+from paper_2609_16648_amd import gm, layout
 
 pytestmark = pytest.mark.gpu
 
@@ -280,6 +280,55 @@ def test_attention(name, lens, N, page, n_nodes):
     need_gpu()
     _check_attention(SHAPES[name], lens, N, page, len(lens) + N, n_nodes,
                      parts=0.0 if SHAPES[name].dtype == "f32" else 2.0 ** -16)
+
+
+@pytest.mark.parametrize("name,N,B", [("mqa16", 9, 1100), ("mqa16", 5, 700), ("qwen", 9, 300), ("qwen", 2, 300)])
+def test_attention_many_sequences(name, N, B):
+    """More sequences than a workgroup has threads, one and two KV heads per workgroup, four, and small trees."""
+    need_gpu()
+    lens = np.random.default_rng(B).integers(0, 40, B).tolist()
+    lens[255:258] = [17, 0, 16]
+    _check_attention(SHAPES[name], lens, N, 16, B, parts=2.0 ** -16)
+
+
+@pytest.mark.parametrize("heads,kv,N,lens,page", [
+    (72, 24, 64, [9000, 8007, 100, 17900, 0, 9000, 42011], 64),      # 192 rows: one KV head per workgroup
+    (72, 24, 33, [39000, 8007, 100, 77900, 52000], 16),              # 99 rows: two
+    (42, 42, 40, [39000, 8007, 100, 50001], 16),                     # 40 rows: four
+    (42, 42, 8, [9000, 8007, 100, 50001], 32),                       # a small tree
+])
+def test_attention_long_ranges(heads, kv, N, lens, page):
+    """Ranges of many tiles per workgroup, over several of its windows; a few heads are compared."""
+    need_gpu()
+    shape = dataclasses.replace(BF16, n_heads=heads, n_kv_heads=kv)
+    B, D, G, total = len(lens), 128, heads // kv, [m + N for m in lens]
+    cache = gm.PagedCache(shape, 1, lens, total, page_size=page, seed=N, fill="empty")
+    g = torch.Generator(device="cuda").manual_seed(N)
+    for p in cache.k + cache.v:
+        p.copy_(torch.randn(p.shape, generator=g, device="cuda", dtype=torch.bfloat16))
+    q = _rand(shape, B, N, heads, D, seed=N + 1)
+    masks = _masks(_trees(B, N, N))[0]
+    out = torch.full((B, N, heads, D), 3.0, dtype=torch.bfloat16, device="cuda")
+    gm.tree_attention(gm.model_config(shape), cache, 0, t32(q, torch.bfloat16), _bits(masks), out, gm.Workspace())
+    for b in range(B):
+        for h in (0, kv - 1):
+            kvs = []
+            for which in ("k", "v"):
+                page_ids, elem = layout.element_index(np.arange(total[b]), cache.block_table_host[b], page, D, which)
+                pool = cache._pool(0, which)[:, h]
+                kvs.append(pool[torch.from_numpy(page_ids).cuda()[:, None], torch.from_numpy(elem).cuda()]
+                           .float().cpu().numpy()[:, None])
+            rows = slice(h * G, (h + 1) * G)
+            k, v = (x[:, 0].astype(np.float64) for x in kvs)
+            sc = np.einsum("ihd,td->iht", q[b][:, rows].astype(np.float64), k, optimize=True) / np.sqrt(D)
+            sc[:, :, lens[b]:] = np.where(masks[b][:, None], sc[:, :, lens[b]:], -np.inf)
+            p = np.exp(sc - sc.max(-1, keepdims=True))
+            p /= p.sum(-1, keepdims=True)
+            want, mag = p @ v, p @ np.abs(v)
+            s_abs = np.abs(q[b][:, rows]).max((0, 1)).sum() * np.abs(kvs[0]).max() / np.sqrt(D)
+            tol = (2 * D * U * s_abs + 2.0 ** -16 + (total[b] / 16 + 64) * U) * mag + 2.0 ** -8 * np.abs(want)
+            over = np.abs(out[b][:, rows].float().cpu().numpy() - want) - tol
+            assert over.max() <= 0, (b, h, over.max())
 
 
 @pytest.mark.parametrize("name,N", [("qwen", 8), ("qwen", 40), ("f32", 6)])
