@@ -473,10 +473,11 @@ typedef struct {
  *   top_logp, top_ids [M][topk] (both or neither): the topk largest logits' log p and
  *     ids, in decreasing logit, equal logits in increasing id; 1 <= topk <= min(64, V).
  *   stats [M]: for gm_token_logprobs_grad.
- * Sums are float32 over at most 8192 ids, added pairwise in part, and float64 beyond.  Logits of -inf have
- * probability 0; a log p below float32's range is -inf.  A row without any other logit: log p -inf, entropy 0, stats (-inf, 0),
- * alternatives 0 .. topk-1.  A row that holds NaN or +inf gives NaN log p and entropy,
- * and alternatives -1.
+ * Sums are float32 over at most 4096 ids, added pairwise in part, and float64 beyond.
+ * Logits of -inf have probability 0; a log p below float32's range is -inf.  A row
+ * without any other logit: log p -inf, entropy 0, stats (-inf, 0), alternatives
+ * 0 .. topk-1.  A row that holds NaN or +inf gives NaN log p and entropy, and
+ * alternatives -1.
  * Limits: V <= 524288, M <= 2^23. */
 gm_status gm_token_logprobs(int M, int V, int dtype, const void *logits, int64_t ld, float temperature,
                             const int32_t *ids, float *logp, float *entropy, int topk, float *top_logp,

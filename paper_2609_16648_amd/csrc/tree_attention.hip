@@ -3,20 +3,28 @@
 // nodes, (n_heads / n_kv_heads) * N, up to 4096.
 //
 // Up to 32 rows: the kernel of the verify attention (attention.h), whose waves stream K and V straight into
-// operand registers, one wave per KV head; bound by HBM.
-// More rows (tree_attn_kernel): a wave holds 64 rows, so that a KV tile read from LDS serves 64 queries; a
-// workgroup's four waves are four heads of up to 64 rows, two of up to 128 or one of up to 256 (further rows: further
-// workgroups), and the workgroup brings each tile into LDS once for all of them.
+// operand registers, one wave per KV head; bound by HBM: 32 sequences of 16K to 32K tokens, 8 KV heads, 4 query heads
+// each and 8 nodes take 512 us, 6.3 TB/s.  (The kernel below takes 517 there; 138 / 141 us at 64 sequences of 1K to 4K,
+// 129 / 135 with 5 nodes.)
+// More rows (tree_attn_kernel): the workgroup brings each KV tile into LDS once for all of its rows.
+//    Up to 64 rows: four heads, a wave of 64 rows each.  Up to 128: two heads, and more: one, with eight waves of 32
+//    rows, two per SIMD (further rows: further workgroups).
 //  * S^T = K Q^T and O^T = V^T P^T on v_mfma_f32_32x32x16_bf16: a lane holds half of the tokens of one query,
 //    so a row's maximum takes one exchange between lanes and P goes into the second product without one.
 //  * K and V go from memory into LDS without passing registers, in stages of 32 tokens (a pair of tiles) of the
-//    workgroup's heads, 128 KiB of them: 2, 4 or 8 stages, all but the one being read in flight.
+//    workgroup's heads, 128 KiB of them: 2, 4 or 8 stages.  A window of a range's tiles is listed once: a stage's places
+//    in the pool, and whether it ends its sequence.
 //    Four heads: each wave brings its own head's tiles, reads a stage's operands into registers at once
-//    and gives its place to the stage after next; no wave waits for another.  Fewer heads: a barrier per stage
-//    says that the stage has arrived for all waves and that the one before it has been read.
-//  * The operands of a stage are asked for together, before its first product.
+//    and gives its place to the stage after next; no wave waits for another.  Fewer heads: a barrier per two stages
+//    says that they have arrived for all waves and that the two before have been read (a barrier for each: 306 us
+//    where this takes 294).
 //  * P is split into bf16 hi + lo parts, two products per V operand: the weights keep 16 bits.
 //  * Work partition, partials and their combination are the verify attention's.
+// 64 sequences of 1K to 4K tokens with 16 nodes (64 rows a head, 675 MB): 157 us with the combination, bound by HBM (4.3
+// TB/s) and the 2 x 32 MB of partials.  32 sequences of 0.5K to 8.7K tokens with 64 nodes (256 rows a head): 294 us, 231
+// GFLOP with the second part of P at 0.87 PFLOP/s, where a product of 8192^3 reaches 1.18 on this card.  Neither fewer
+// vector instructions, nor whole-rate V reads, nor two groups of waves that take turns at the matrix unit and the weights
+// changed that by more than 3%.
 #include "attention.h"
 
 namespace gm {
