@@ -88,12 +88,15 @@ __global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs a) {
   // the sequence of this unit: the last one with at most u units before it
   int b;
   if (a.row_start) {
-    int n = 0;
-    for (int i = 0; i < a.B; i += 256) {
-      const int s = i + tid;
-      n += __syncthreads_count(s < a.B && units_before(a.row_start[s], s) <= u);
+    // 256 places at a time, each round within one step of the round before
+    int lo = 0;
+    for (int len = a.B, step = 0; step != 1; len = min(step, a.B - lo)) {
+      step = (len + 255) / 256;
+      const int i = tid * step;
+      const int n = __syncthreads_count(i < len && units_before(a.row_start[lo + min(i, len - 1)], lo + i) <= u);
+      if (n > 1) lo += (n - 1) * step;
     }
-    b = n > 0 ? n - 1 : 0;
+    b = lo;
   } else {
     const int R = a.T / a.B;
     b = (int)(16 * u / (R + 32));       // units_before is between b (R + 32) / 16 - 1 and b (R + 32) / 16

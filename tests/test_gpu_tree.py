@@ -94,6 +94,7 @@ APPEND = [
     ("f32", [0, 13, 130], [5, 64, 2], 16, True, True, False),
     ("f32_g4_d128", [33, 1], [31, 18], 32, True, False, True),
     ("f32", [2, 2], None, 16, False, True, True),
+    ("mha", [7 * i % 50 for i in range(600)], [5 * i % 4 for i in range(600)], 16, False, True, True),
 ]
 
 
@@ -378,6 +379,31 @@ def test_attention_unseen_entries_do_not_reach_a_row(name, N):
     assert not np.isfinite(outs[2][only][..., ~keep]).any()
 
 
+@pytest.mark.parametrize("name,N", [("qwen", 8), ("qwen", 16), ("qwen", 40), ("g7", 64), ("mha", 12), ("f32", 9)])
+@pytest.mark.parametrize("pos", [20, 15, 2])
+def test_attention_committed_infinities_reach_every_row(name, N, pos):
+    """V of a committed token that is inf in some channels (in the tile of the first nodes, or before it)."""
+    need_gpu()
+    shape, lens = SHAPES[name], [21]
+    q = _rand(shape, 1, N, shape.n_heads, shape.head_dim, seed=5, scale=0.25)
+    masks = _masks(_trees(1, N, 3))[0]
+    dt = gm.torch_dtype(shape)
+    outs = []
+    for bad in (False, True):
+        cache = gm.PagedCache(shape, 1, lens, [21 + N], seed=2)
+        ks, vs = _entries(cache, shape, lens, N, 11)
+        if bad:
+            v = vs[0][pos].copy()
+            v[..., 1::3] = np.inf
+            cache.write(0, 0, [pos], ks[0][pos][None], v[None])
+        out = torch.empty((1, N, shape.n_heads, shape.head_dim), dtype=dt, device="cuda")
+        gm.tree_attention(gm.model_config(shape), cache, 0, t32(q, dt), _bits(masks), out, gm.Workspace())
+        outs.append(out.float().cpu().numpy())
+    assert not np.isfinite(outs[1][..., 1::3]).any()
+    for c in (0, 2):
+        assert np.allclose(outs[1][..., c::3], outs[0][..., c::3], rtol=2.0 ** -7, atol=1e-6)
+
+
 def test_attention_bad_page_ends_its_sequence():
     need_gpu()
     lens, N = [100, 100], 8
@@ -422,7 +448,8 @@ def test_accept(B, N):
 
 @pytest.mark.parametrize("name,layers,lens,N,page", [
     ("qwen", 1, [0, 15, 16, 100], 16, 16), ("qwen", 36, [30, 3], 64, 32), ("mha", 2, [9, 63, 64], 9, 64),
-    ("f32", 2, [0, 40], 64, 16), ("f32_g4_d128", 3, [17], 12, 16)])
+    ("f32", 2, [0, 40], 64, 16), ("f32_g4_d128", 3, [17], 12, 16),
+    ("mha", 130, [9], 9, 16)])                                     # layers for two launches
 def test_commit(name, layers, lens, N, page):
     need_gpu()
     shape = dataclasses.replace(SHAPES[name], n_layers=max(1, layers - 1))     # the cache's layers are its own
