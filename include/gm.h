@@ -478,7 +478,7 @@ typedef struct {
  * without any other logit: log p -inf, entropy 0, stats (-inf, 0), alternatives
  * 0 .. topk-1.  A row that holds NaN or +inf gives NaN log p and entropy, and
  * alternatives -1.
- * Limits: V <= 524288, M <= 2^23. */
+ * Limits: V <= 524288, M <= 2^23, temperature >= 1e-37. */
 gm_status gm_token_logprobs(int M, int V, int dtype, const void *logits, int64_t ld, float temperature,
                             const int32_t *ids, float *logp, float *entropy, int topk, float *top_logp,
                             int32_t *top_ids, gm_token_stats *stats, void *ws, size_t ws_bytes, int32_t *dev_err,

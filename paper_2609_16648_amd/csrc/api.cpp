@@ -552,6 +552,8 @@ gm_status check_rows(int M, int V, int dtype, int64_t ld, float temperature) {
   if (dtype != GM_F32 && dtype != GM_BF16) return fail(GM_ERR_INVALID_ARG, "unknown dtype %d", dtype);
   if (ld < V) return fail(GM_ERR_INVALID_ARG, "rows of %d logits are %lld apart", V, (long long)ld);
   if (!(temperature > 0.f) || !isfinite(temperature)) return fail(GM_ERR_INVALID_ARG, "temperature must be > 0 and finite");
+  // (its reciprocal is a float32 factor of the kernels)
+  if (temperature < 1e-37f) return fail(GM_ERR_UNSUPPORTED, "temperature %g is less than 1e-37", (double)temperature);
   return GM_OK;
 }
 }  // namespace

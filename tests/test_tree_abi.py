@@ -101,6 +101,7 @@ def test_token_logprobs_rejects():
     assert _lp(V=524289, ld=524289) == U and _lp(M=(1 << 23) + 1) == U
     for T in (0.0, -1.0, float("nan"), float("inf")):
         assert _lp(T=T) == A and "temperature" in gm.last_error()
+    assert _lp(T=9e-38) == U and _lp(T=1e-45) == U
     assert _lp(z=None) == A and _lp(ids=None) == A
     assert _lp(topk=4, tl=FAKE) == A and _lp(topk=4, ti=FAKE) == A
     assert _lp(topk=0, tl=FAKE, ti=FAKE) == A and _lp(topk=65, tl=FAKE, ti=FAKE) == A
