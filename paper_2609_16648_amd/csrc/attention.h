@@ -30,6 +30,7 @@
 #pragma once
 
 #include <atomic>
+#include <type_traits>
 
 #include "common.h"
 #include "tree.h"
@@ -578,6 +579,9 @@ __global__ __launch_bounds__(64 * kAttnWavesPerGroup) void attn_mfma_kernel(Attn
 // row, group i taking batches i, i + SP, ..; their results meet in LDS in group order.
 // SP = 16 where few sequences are cut into many partials each: the pass is a chain of
 // load round trips (one sequence in 126 partials: 42 us with one group, 8.5 with sixteen).
+// One group stops at the last partial (it is the same for the whole block: 20 us against 22 for 32 sequences of 2 to 3
+// partials of 2048 rows, 9.3 against 11.4 for one of 32); sixteen, where it differs within a wave, load the last one
+// again (9.2 against 10 where they stop too).
 constexpr int kCombineBatch = 8;
 
 template <int SP>
@@ -610,11 +614,12 @@ __global__ __launch_bounds__(SP > 1 ? 32 * SP : 256) void attn_combine_kernel(At
     M = mn;
   };
   if (i < blen && T > 0) {
-    for (int p0 = pf + kCombineBatch * sp; p0 <= pl; p0 += kCombineBatch * SP) {
+    auto batch = [&](int p0, auto stop) {      // stop: nothing is loaded past the last partial
       float2 ml[kCombineBatch];
       float4 o[kCombineBatch];
 #pragma unroll
       for (int u = 0; u < kCombineBatch; ++u) {
+        if (decltype(stop)::value && p0 + u > pl) break;
         const int p = min(p0 + u, pl);
         const long pr = ((long)(p + b) * a.n_kv + kvh) * a.rows_pad + r;
         ml[u] = a.part_ml[pr];
@@ -623,12 +628,17 @@ __global__ __launch_bounds__(SP > 1 ? 32 * SP : 256) void attn_combine_kernel(At
 #pragma unroll
       for (int u = 0; u < kCombineBatch; ++u) {
         const int p = p0 + u;
+        if (decltype(stop)::value && p > pl) break;
         if (p > pl || ml[u].x == -INFINITY) continue;
         // ranges are empty only where there are more of them than tiles (asked first: two 64-bit
         // divisions per partial cost 3 sequences in 45 partials each 4 us of 31)
         if (TT < P && part_begin(p, TT, P) == part_begin(p + 1, TT, P)) continue;
         merge(ml[u].x, ml[u].y, o[u]);
       }
+    };
+    for (int p0 = pf + kCombineBatch * sp; p0 <= pl; p0 += kCombineBatch * SP) {
+      if (SP == 1 && p0 + kCombineBatch - 1 > pl) batch(p0, std::true_type());
+      else batch(p0, std::false_type());
     }
   }
   if constexpr (SP > 1) {
