@@ -44,14 +44,14 @@ template <int n> __device__ __forceinline__ void load_to_lds(uint32_t lds, const
         "global_load_lds_dwordx4 %2, %1 nt\n\t"
         "global_load_lds_dwordx4 %2, %1 offset:1024 nt\n\t"
         "global_load_lds_dwordx4 %2, %1 offset:2048 nt\n\t"
-        "global_load_lds_dwordx4 %2, %1 offset:3072 nt" ::"s"(lds), "s"(src), "v"(off)
-        : "memory");
+        "global_load_lds_dwordx4 %2, %1 offset:%3 nt" ::"s"(lds), "s"(src), "v"(off), "n"(3 * 1024)
+        : "memory", "m0");
   else
     asm volatile(
         "s_mov_b32 m0, %0\n\ts_nop 0\n\t"
         "global_load_lds_dwordx4 %2, %1 nt\n\t"
         "global_load_lds_dwordx4 %2, %1 offset:1024 nt" ::"s"(lds), "s"(src), "v"(off)
-        : "memory");
+        : "memory", "m0");
 }
 // until at most n vector memory operations of this wave are under way (older ones complete first)
 template <int n> __device__ __forceinline__ void wait_vm() {
