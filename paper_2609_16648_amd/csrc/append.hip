@@ -12,7 +12,7 @@
 // quads whole where units of 16 rows would not.)  A workgroup takes the rotations of its 16
 // tokens once, into LDS, for all heads; its four waves take the heads in turn, a wave 16 tokens
 // of one q or k head, or of the 2 (head_dim 128) or 4 (64) v heads that fill its lanes.
-// Bound by HBM: every row is read once and written once.  32768 rows of 32 + 8 + 8 bf16 heads of 128 (802 MB) take
+// Bound by HBM: every row is read once and written once.  32.6K rows of 32 + 8 + 8 bf16 heads of 128 (802 MB) take
 // 189 us, 4.2 TB/s, where a copy of 2 GiB reaches 4.9; V through LDS instead of the register transpose took 204.
 //
 // Precision: the angle in float64 as a fraction of a turn (positions reach 32K and beyond, where a
@@ -249,7 +249,7 @@ void launch_kv_append(const AppendArgs &a, hipStream_t s) {
   TraceScope ts("kv_append", s);
   const int tasks = a.n_heads + a.n_kv + (a.n_kv * a.head_dim / 4 + 63) / 64;
   // Few units: their heads are dealt to more workgroups, until about 2048 of them (eight per CU).  Measured with 2048 /
-  // 8192 / 16384, bf16, 32 q and 8 KV heads of 128: 32 prompts of 1024 rows 189 / 207 / 200 us, 256 trees of 4 nodes
+  // 8192 / 16384, bf16, 32 q and 8 KV heads of 128: 32 prompts of 37 to 2001 rows 189 / 207 / 200 us, 256 trees of 4 nodes
   // 22 / 30 / 30, 64 trees of 16 nodes 14.6 / 14.8 / 14.3: more workgroups repeat the rotations and the table reads.
   int y = (int)((2048 + units - 1) / units);
   const int most = (tasks + 3) / 4;
