@@ -471,7 +471,11 @@ __global__ __launch_bounds__(tree_block(HG)) void tree_attn_kernel(AttnK a) {
   }
 }
 
-// Row tiles of a KV head: up to two go to attn_mfma_kernel; more, in 64s, to waves of tree_attn_kernel.
+// Up to 32 rows of a KV head go to attn_mfma_kernel, more to tree_attn_kernel with as many heads per workgroup as give a
+// head's rows waves of their own.  Measured (us, combination included; 64 sequences of 1K to 4K tokens with 8 KV heads):
+// 48 and 64 rows with four heads 157 and 162, two 198 and 199; 96 and 128 rows with two 203 and 215, one 286 and 303,
+// four and a workgroup per 64 rows 237 and 237; 256 rows (32 sequences of 0.5K to 8.7K) with one 304, four 350.  One
+// sequence of 4001 tokens and 64 rows alone is faster with two heads (24 against 30).
 struct TreeGeom {
   bool wide;
   int heads_per_group, groups, row_groups, rows_pad, block, rt;
